@@ -479,6 +479,151 @@ wam_status wam_denoise_chunk(const wam_model* m, const wam_step_io* io, const wa
                              void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------------
+ * Serving requests with histories of their own: a KV cache in pages.
+ *
+ * One layer's cache is a pool of n_pages pages of page_size token rows.  A request r owns a
+ * list of pages, row r of a block table: its key j lies in row j % page_size of page
+ * block_table[r][j / page_size].  The four entry points below build the tables on the GPU
+ * from the requests' lengths, write a projection's K and V into the pages, attend over
+ * them, and attend to other sequences (text, images) of per-request lengths.
+ *
+ * Ragged rows  The requests' rows lie in one [T] row range: request r has rows
+ *   [q_start[r], q_start[r] + q_len[r]), where q_start holds R + 1 non-decreasing
+ *   values and q_len may be NULL (q_start[r+1] - q_start[r]); with q_len given, rows may lie between a
+ *   request's last and the next one's first (a padded batch; q_len[r] is cut to the room
+ *   there is).  Rows outside every request are neither read nor written.
+ * Device values  Lengths, starts, tables and slots are int32 DEVICE arrays (4-byte
+ *   aligned), so that a captured graph serves other requests when they change.  The host
+ *   cannot check them.  What they say is bounded on the device: starts and lengths are
+ *   cut to the T (S) rows that the call names, keys to max_kv (max_k) and to the table's
+ *   width, and a page id outside [0, n_pages) is an absent page, whose keys no query sees.
+ *   So no value in them makes a kernel leave the caller's buffers.
+ *
+ * wam_paged_cache
+ *   k, v       [n_pages][page_size][Hkv][Dh] bf16, row (page, token, head) at page *
+ *              page_stride + token * tok_stride + head * head_stride (elements, multiples
+ *              of 8; the Dh values contiguous); so pages of [Hkv][page_size][Dh] and K and V as the
+ *              halves of one buffer are possible too.
+ *   k_exp      NULL, or (Dh = 128) an FP8 cache in the formats of wam_rope_qkv_fp8: k and v
+ *              hold E4M3 codes (strides in bytes, multiples of 128), k_exp uint32 block exponents, one
+ *              per row, addressed with the code strides divided by 128; v = code * v_scale.
+ *   page_size is a multiple of 16; a page's rows span less than 2 GiB; n_pages *
+ *   page_size < 2^31.
+ * ------------------------------------------------------------------------------ */
+typedef struct {
+  void *k, *v, *k_exp;
+  int64_t page_stride, tok_stride, head_stride;
+  int32_t n_pages, page_size, Hkv, Dh;
+  float v_scale;
+} wam_paged_cache;
+
+/* wam_page_plan — block tables and slot maps from request lengths, on the GPU.
+ *
+ * Request r keeps the first cache_len[r] tokens of its history and gets new_len[r] new ones
+ * (cache_len = new_len = 0: it has ended), so it needs need = ceil((cache_len + new_len) /
+ * page_size) pages (at most max_pages, the width of its table row).  It holds held[r] of them:
+ * block_table[r][0 .. held[r]).  free_list [n_pages] is a stack of n_free[0] free pages.
+ *   1. Surplus pages (entries [need, held)) are put on the stack, in order of requests and of
+ *      entries within one.
+ *   2. The pages that are missing (entries [held, need)) are taken from its top, in the same order; an
+ *      entry for which the stack holds no page any more becomes -1 (status[0] counts them).
+ * Written: block_table entries [held, need); free_list entries [n_free, n_free_out); and
+ *   held_out [R]   pages that each request holds now;   n_free_out [1]
+ *   q_start [R+1]  first row of each request among the new tokens, packed in request order
+ *                  (cut to T; new tokens past T are left out)
+ *   kv_len [R]     cache_len + the new tokens that have a row
+ *   slots [T]      page * page_size + row of each new token's place in the cache; -1 for rows
+ *                  past the last request and tokens without a page
+ *   token_pos [T]  optional: each new token's position in its request, -1 past the last one
+ *   status [4]     pages missing; pages past the tables' width; new tokens past T;
+ *                  invalid inputs (negative lengths, held outside [0, max_pages], n_free
+ *                  outside [0, n_pages]: each is cut to its range)
+ * held_out and n_free_out must not overlap held and n_free (every workgroup reads those); with
+ * the counters kept apart, a call repeated on the same inputs gives the same result.
+ * R <= WAM_PLAN_MAX_REQUESTS, R * max_pages < 2^31.  No workspace; deterministic. */
+#define WAM_PLAN_MAX_REQUESTS 4096
+typedef struct {
+  int32_t R, T, page_size, n_pages, max_pages;
+  int64_t table_stride; /* entries between the table's rows, >= max_pages */
+} wam_page_plan_desc;
+wam_status wam_page_plan(const wam_page_plan_desc* desc, const int32_t* cache_len, const int32_t* new_len,
+                         const int32_t* held, const int32_t* n_free, int32_t* block_table, int32_t* free_list,
+                         int32_t* held_out, int32_t* n_free_out, int32_t* q_start, int32_t* kv_len,
+                         int32_t* slots, int32_t* token_pos, int32_t* status, hipStream_t stream);
+
+/* wam_rope_qkv_paged — rotary positions with one to four axes, and the append to a paged
+ * cache: wam_rope_qkv for tokens of any requests, with the angles formed on the GPU.
+ *
+ * qkv [T] rows (stride qkv_tok_stride) of q [Hq][Dh] | k [Hkv][Dh] | v [Hkv][Dh] bf16; pos [T][n_axes]
+ * int32.  Pair i (of pairs[a]) of axis a turns by pos[t][a] * theta^(-i / pairs[a]); the axes'
+ * pairs follow each other, n = sum of pairs <= Dh / 2.  Pair number p is dims (2p, 2p + 1), or
+ * (p, p + n) with halves = 1 (then n must be a multiple of 8, of 32 for an FP8 cache); dims from
+ * 2n on are kept.  (The split of wam_rope_tables is pairs = (Dh/2 - 2 floor(Dh/6), floor(Dh/6),
+ * floor(Dh/6)).)  Angles are formed in fp64 and reduced there, so a far position is as exact as a
+ * near one; the rotation is in fp32, rounded once.
+ * q_out [T] rows (stride q_tok_stride) of [Hq][Dh] bf16 receives the rotated q (NULL: q is not
+ * needed, as in a cache-update pass); the rotated k and v go to row slots[t] % page_size of page
+ * slots[t] / page_size of the cache (FP8 cache: encoded as by wam_rope_qkv_fp8).  A token
+ * whose slot lies outside [0, n_pages * page_size) is skipped: nothing of it is written. */
+#define WAM_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t T, Hq, n_axes;
+  int32_t pairs[WAM_ROPE_MAX_AXES];
+  int32_t halves;
+  double theta;
+  int64_t qkv_tok_stride, q_tok_stride;
+} wam_rope_paged_desc;
+wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_cache* cache, const void* qkv,
+                              const int32_t* pos, const int32_t* slots, void* q_out, hipStream_t stream);
+
+/* wam_attn_paged — softmax attention of ragged new tokens over a paged cache.
+ *
+ * Request r has n = q_len[r] query rows, which are the last n of its kv_len[r] tokens (their K
+ * and V are in the cache already): row i has position p = kv_len[r] - n + i.  It sees the keys
+ * j < kv_len[r] with
+ *   chunk = 0   all of them;
+ *   chunk = c   j < (floor(p / c) + 1) * c: the chunks up to its own, every chunk c tokens
+ *               (Appendix C, Figure 10b; c = 1 is causal attention).
+ * A row that sees no key (kv_len = 0, absent pages, p < 0) gives 0.  Query head h reads KV head
+ * h / (Hq / Hkv); Hq must be a multiple of Hkv.  scale <= 0 selects 1/sqrt(Dh); Dh 64 or 128.
+ * q, o: [T] rows of [Hq][Dh] bf16 at their token strides (multiples of 8); o must not overlap q
+ * or the cache.  With an FP8 cache K and V are decoded (exactly, to bf16; v_scale is applied in
+ * fp32) and q stays bf16.  Rows of the cache that hold no key of a request are not used,
+ * whatever they hold; a NaN or infinity in V of a key that only some of a request's rows see may
+ * reach its other rows.
+ * max_kv bounds kv_len (longer ones are cut); it, R and T choose how the key axis is split, and
+ * with them the rounding, so results are bitwise the same for the same sizes whatever the
+ * device values' order (no atomics).  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes
+ * (may be 0: then ws may be NULL), 256-byte aligned; calls that may overlap in time need
+ * workspaces of their own. */
+typedef struct {
+  int32_t R, T, Hq, max_pages, max_kv, chunk;
+  int64_t table_stride;
+  int64_t q_tok_stride, o_tok_stride;
+  float scale;
+} wam_attn_paged_desc;
+size_t wam_attn_paged_workspace_bytes(const wam_attn_paged_desc* desc, const wam_paged_cache* cache);
+wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache* cache, const void* q,
+                          const int32_t* block_table, const int32_t* q_start, const int32_t* q_len,
+                          const int32_t* kv_len, void* o, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* wam_attn_cross — softmax attention to another sequence's states, of a length per request:
+ * every row of request r sees all k_len[r] key rows from row k_start[r] of k and v (0 where there
+ * are none).  k, v: [S] rows of [Hkv][Dh] bf16 sharing kv_tok_stride (they may be halves of one buffer).
+ * k_len NULL: k_start holds R + 1 values and request r's keys end where the next one's begin;
+ * with k_len, k_start holds R values in any order, and requests may share key rows.  Queries,
+ * heads, scale, max_k, workspace and determinism as for wam_attn_paged. */
+typedef struct {
+  int32_t R, T, S, Hq, Hkv, Dh, max_k;
+  int64_t q_tok_stride, kv_tok_stride, o_tok_stride;
+  float scale;
+} wam_attn_cross_desc;
+size_t wam_attn_cross_workspace_bytes(const wam_attn_cross_desc* desc);
+wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const void* k, const void* v,
+                          const int32_t* q_start, const int32_t* q_len, const int32_t* k_start,
+                          const int32_t* k_len, void* o, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------------
  * Pieces of the step, exported for testing each kernel on its own.
  * ------------------------------------------------------------------------------ */
 

@@ -34,7 +34,8 @@ EXPORTED = (
     "wam_chunk_positions", "wam_rope_tables", "wam_attn_blockcausal_fp8", "wam_quantize_mx_fp8",
     "wam_quantize_scaled_fp8", "wam_rope_qkv_fp8", "wam_unipc_plan", "wam_unipc_step",
     "wam_cosine_similarity_noalloc", "wam_adaln_ln_mod_fp8", "wam_gemm_fp8_mx",
-    "wam_attn_blockcausal_mx", "wam_attn_blockcausal_fp8_mx",
+    "wam_attn_blockcausal_mx", "wam_attn_blockcausal_fp8_mx", "wam_page_plan", "wam_rope_qkv_paged",
+    "wam_attn_paged_workspace_bytes", "wam_attn_paged", "wam_attn_cross_workspace_bytes", "wam_attn_cross",
 )
 
 _vp, _fp, _i32, _i64, _sz = C.c_void_p, C.POINTER(C.c_float), C.c_int32, C.c_int64, C.c_size_t
@@ -128,6 +129,34 @@ class wam_gemm_desc(C.Structure):
                 ("gate_a", _vp), ("gate_v", _vp), ("gate_stride", _i64), ("gate_rows", _i32)]
 
 
+class wam_paged_cache(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_exp", _vp), ("page_stride", _i64), ("tok_stride", _i64),
+                ("head_stride", _i64), ("n_pages", _i32), ("page_size", _i32), ("Hkv", _i32), ("Dh", _i32),
+                ("v_scale", C.c_float)]
+
+
+class wam_page_plan_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "page_size", "n_pages", "max_pages")] + [("table_stride", _i64)]
+
+
+WAM_PLAN_MAX_REQUESTS, WAM_ROPE_MAX_AXES = 4096, 4
+
+
+class wam_rope_paged_desc(C.Structure):
+    _fields_ = [("T", _i32), ("Hq", _i32), ("n_axes", _i32), ("pairs", _i32 * WAM_ROPE_MAX_AXES), ("halves", _i32),
+                ("theta", C.c_double), ("qkv_tok_stride", _i64), ("q_tok_stride", _i64)]
+
+
+class wam_attn_paged_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "Hq", "max_pages", "max_kv", "chunk")] + \
+               [("table_stride", _i64), ("q_tok_stride", _i64), ("o_tok_stride", _i64), ("scale", C.c_float)]
+
+
+class wam_attn_cross_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "S", "Hq", "Hkv", "Dh", "max_k")] + \
+               [("q_tok_stride", _i64), ("kv_tok_stride", _i64), ("o_tok_stride", _i64), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -143,7 +172,8 @@ def lib():
         for name in ("wam_block_workspace_bytes", "wam_step_workspace_bytes", "wam_update_workspace_bytes",
                      "wam_cosine_workspace_bytes", "wam_denoise_workspace_bytes",
                      "wam_time_embed_workspace_bytes", "wam_text_proj_workspace_bytes",
-                     "wam_embed_workspace_bytes", "wam_head_workspace_bytes"):
+                     "wam_embed_workspace_bytes", "wam_head_workspace_bytes", "wam_attn_paged_workspace_bytes",
+                     "wam_attn_cross_workspace_bytes"):
             getattr(L, name).restype = _sz
         L.wam_block_workspace_bytes.argtypes = [C.POINTER(wam_dims), _i32, _i32, _i32]
         L.wam_step_workspace_bytes.argtypes = [C.POINTER(wam_model), C.POINTER(wam_step_io)]
@@ -195,6 +225,12 @@ def lib():
         L.wam_unipc_plan.argtypes = [_fp, _i32, _i32, C.POINTER(wam_unipc_coef)]
         L.wam_unipc_step.argtypes = [C.POINTER(wam_flow_dims), _vp, _vp, _vp, _vp, _vp, C.POINTER(_vp), _i32,
                                      C.POINTER(wam_unipc_coef), _vp, _vp, _vp, _vp]
+        L.wam_page_plan.argtypes = [C.POINTER(wam_page_plan_desc)] + [_vp] * 14
+        L.wam_rope_qkv_paged.argtypes = [C.POINTER(wam_rope_paged_desc), C.POINTER(wam_paged_cache)] + [_vp] * 5
+        L.wam_attn_paged_workspace_bytes.argtypes = [C.POINTER(wam_attn_paged_desc), C.POINTER(wam_paged_cache)]
+        L.wam_attn_paged.argtypes = [C.POINTER(wam_attn_paged_desc), C.POINTER(wam_paged_cache)] + [_vp] * 7 + [_sz, _vp]
+        L.wam_attn_cross_workspace_bytes.argtypes = [C.POINTER(wam_attn_cross_desc)]
+        L.wam_attn_cross.argtypes = [C.POINTER(wam_attn_cross_desc)] + [_vp] * 9 + [_sz, _vp]
         for name in EXPORTED[2:]:
             if not name.endswith("_bytes"):
                 getattr(L, name).restype = C.c_int
@@ -421,6 +457,87 @@ def wam_rope_qkv(qkv, cos_t, sin_t, q_out, k_cache, v_cache, row0, H, Dh, stream
     B, L = qkv.shape[0], qkv.shape[1]
     _check(lib().wam_rope_qkv(B, L, H, Dh, _p(qkv), _p(cos_t), _p(sin_t), _p(q_out), _p(k_cache),
                               _p(v_cache), k_cache.shape[1], row0, _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------
+# the KV cache in pages
+# ------------------------------------------------------------------------------------------
+def make_paged_cache(k, v, k_exp=None, v_scale=0.0) -> wam_paged_cache:
+    """One layer's pages: k, v [n_pages, page_size, Hkv, Dh] views (strides taken from the tensors), bf16, or
+    uint8 E4M3 codes with k_exp [n_pages, page_size, Hkv] int32 block exponents and v_scale."""
+    n_pages, page_size, Hkv, Dh = k.shape
+    if v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("k and v must share shape and strides")
+    if k.stride(3) != 1:
+        raise ValueError("a row's Dh values must be contiguous")
+    if k_exp is not None and any(e * Dh != s for e, s in zip(k_exp.stride(), k.stride())):
+        raise ValueError("exponent strides must be the code strides / Dh")
+    c = wam_paged_cache(k=_p(k), v=_p(v), k_exp=_p(k_exp), page_stride=k.stride(0), tok_stride=k.stride(1),
+                        head_stride=k.stride(2), n_pages=n_pages, page_size=page_size, Hkv=Hkv, Dh=Dh, v_scale=v_scale)
+    c._keep = (k, v, k_exp)
+    return c
+
+
+def wam_page_plan(cache_len, new_len, held, n_free, block_table, free_list, held_out, n_free_out, q_start, kv_len,
+                  slots, status, page_size: int, token_pos=None, stream=None):
+    """All int32 device tensors: cache_len, new_len, held, held_out, kv_len [R]; n_free, n_free_out [1];
+    block_table [R, max_pages]; free_list [n_pages]; q_start [R + 1]; slots, token_pos [T]; status [4]."""
+    d = wam_page_plan_desc(block_table.shape[0], slots.shape[0], page_size, free_list.shape[0], block_table.shape[1],
+                           block_table.stride(0))
+    _check(lib().wam_page_plan(C.byref(d), _p(cache_len), _p(new_len), _p(held), _p(n_free), _p(block_table),
+                               _p(free_list), _p(held_out), _p(n_free_out), _p(q_start), _p(kv_len), _p(slots),
+                               _p(token_pos), _p(status), _stream(stream)))
+
+
+def wam_rope_qkv_paged(cache: wam_paged_cache, qkv, pos, slots, q_out, pairs, halves=False, theta=10000.0,
+                       stream=None):
+    """qkv [T, (Hq + 2 Hkv) * Dh] bf16 (row stride from the tensor), pos [T, n_axes] int32 contiguous, slots [T]
+    int32; q_out [T, Hq, Dh] bf16 (token stride from the tensor) or None; pairs: rotated pairs of each axis."""
+    T, n = qkv.shape[0], len(pairs)
+    if pos.shape[1] != n:
+        raise ValueError("pos must have one column per entry of pairs")
+    d = wam_rope_paged_desc(T=T, Hq=qkv.shape[1] // cache.Dh - 2 * cache.Hkv, n_axes=n, halves=int(halves), theta=theta,
+                            qkv_tok_stride=qkv.stride(0), q_tok_stride=0 if q_out is None else q_out.stride(0))
+    d.pairs[:min(n, WAM_ROPE_MAX_AXES)] = pairs[:WAM_ROPE_MAX_AXES]
+    _check(lib().wam_rope_qkv_paged(C.byref(d), C.byref(cache), _p(qkv), _p(pos), _p(slots), _p(q_out),
+                                    _stream(stream)))
+
+
+def wam_attn_paged_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: int, max_kv: int) -> int:
+    d = wam_attn_paged_desc(R=R, T=T, Hq=Hq, max_kv=max_kv)
+    return lib().wam_attn_paged_workspace_bytes(C.byref(d), C.byref(cache))
+
+
+def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, ws=None, max_kv=None, chunk=0, q_len=None,
+                   scale=0.0, stream=None):
+    """q, o [T, Hq, Dh] bf16 (token strides from the tensors); block_table [R, max_pages], q_start [R + 1],
+    kv_len and q_len [R] int32; max_kv (default: what the table's width can hold) bounds kv_len; ws a uint8 device
+    tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
+    T, Hq, _ = q.shape
+    R, width = block_table.shape
+    d = wam_attn_paged_desc(R, T, Hq, width, width * cache.page_size if max_kv is None else max_kv, chunk,
+                            block_table.stride(0), q.stride(0), o.stride(0), scale)
+    _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), _p(q), _p(block_table), _p(q_start), _p(q_len), _p(kv_len),
+                                _p(o), _p(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def wam_attn_cross_workspace_bytes(R: int, T: int, Hq: int, Hkv: int, Dh: int, max_k: int) -> int:
+    d = wam_attn_cross_desc(R=R, T=T, Hq=Hq, Hkv=Hkv, Dh=Dh, max_k=max_k)
+    return lib().wam_attn_cross_workspace_bytes(C.byref(d))
+
+
+def wam_attn_cross(q, k, v, q_start, k_start, o, ws=None, max_k=None, q_len=None, k_len=None, scale=0.0, stream=None):
+    """q, o [T, Hq, Dh] bf16; k, v [S, Hkv, Dh] bf16 views (token strides from the tensors); q_start [R + 1], q_len
+    [R] or None, k_start [R] with k_len [R], or [R + 1] without; max_k (default S) bounds k_len; ws a uint8 device
+    tensor of at least wam_attn_cross_workspace_bytes(R, T, Hq, Hkv, Dh, max_k)."""
+    T, Hq, Dh = q.shape
+    S, Hkv, _ = k.shape
+    if v.stride(0) != k.stride(0):
+        raise ValueError("k and v must share the token stride")
+    d = wam_attn_cross_desc(q_start.shape[0] - 1, T, S, Hq, Hkv, Dh, S if max_k is None else max_k, q.stride(0),
+                            k.stride(0), o.stride(0), scale)
+    _check(lib().wam_attn_cross(C.byref(d), _p(q), _p(k), _p(v), _p(q_start), _p(q_len), _p(k_start), _p(k_len), _p(o),
+                                _p(ws), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def make_dims(d, H, Dh, ffn, n_layers, latent_ch=16, act_dim=16, text_dim=4096, freq_dim=256, eps=1e-6):

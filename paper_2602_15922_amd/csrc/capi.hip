@@ -10,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "capi_check.h"
 #include "kernels.h"
 
 using namespace wam;
@@ -17,6 +18,22 @@ using namespace wam;
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+namespace wam {
+wam_status fail(wam_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return st;
+}
+}  // namespace wam
+
+namespace {
 
 // Inside the denoising loop with DiT caching, every kernel of a step is launched with
 // the loop's device flag (a reused step's kernels return at entry; the decision stays
@@ -32,33 +49,6 @@ const Args& pred(Args& a) {
   return a;
 }
 
-wam_status fail(wam_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_err = buf;
-  return st;
-}
-
-#define CHECK(cond, st, ...) \
-  do {                       \
-    if (!(cond)) return fail(st, __VA_ARGS__); \
-  } while (0)
-
-#define HIPCHECK(expr)                                                              \
-  do {                                                                              \
-    hipError_t e_ = (expr);                                                         \
-    if (e_ != hipSuccess) return fail(WAM_EHIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-#define TRY(expr)                      \
-  do {                                 \
-    wam_status s_ = (expr);            \
-    if (s_ != WAM_OK) return s_;       \
-  } while (0)
-
 // A launch sequence (block, step, update pass, loop) first runs dry: every descriptor of
 // every launch is built and validated, nothing is launched or recorded.  Only if that
 // pass returns WAM_OK does the same sequence run for real, so an invalid argument found
@@ -72,19 +62,6 @@ struct DryScope {
   do {                        \
     if (!t_dry) HIPCHECK(expr); \
   } while (0)
-
-bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-bool al4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
-
-wam_status need_ptr(const void* p, const char* name) {
-  if (!p) return fail(WAM_EINVAL, "%s is NULL", name);
-  if (!al16(p)) return fail(WAM_EINVAL, "%s is not 16-byte aligned", name);
-  return WAM_OK;
-}
-wam_status opt_ptr(const void* p, const char* name) {
-  if (p && !al16(p)) return fail(WAM_EINVAL, "%s is not 16-byte aligned", name);
-  return WAM_OK;
-}
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 

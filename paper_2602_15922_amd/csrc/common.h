@@ -95,6 +95,18 @@ WAM_DEV int mx_exp_biased(float amax) {
   return eb < 0 ? 0 : eb;
 }
 
+// E4M3 codes of 8 values times mul, saturating, round to nearest even.
+WAM_DEV u32x2 e4m3x8(const float* f, float mul) {
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = fminf(fmaxf(f[j] * mul, -448.0f), 448.0f);
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+  return u32x2{(uint32_t)lo, (uint32_t)hi};
+}
+
 // The denoising loop launches a step's kernels with a device flag: while it is > 0 the
 // step reuses an earlier velocity and every workgroup returns at entry.
 WAM_DEV bool skip_step(const int32_t* skip) { return skip != nullptr && *skip > 0; }

@@ -321,17 +321,6 @@ __global__ __launch_bounds__(256) void quant_rows_reg_kernel(int M, int K, const
 // scaling and round to nearest even.  One thread converts 8 elements; the 4 threads of
 // a block (consecutive lanes) share its maximum through two lane exchanges.
 // ---------------------------------------------------------------------------------
-WAM_DEV u32x2 e4m3x8(const float* f, float mul) {
-  float y[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = fminf(fmaxf(f[j] * mul, -448.0f), 448.0f);
-  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
-  return u32x2{(uint32_t)lo, (uint32_t)hi};
-}
-
 // 8 values of one 32-element block -> 8 codes; returns the block's biased exponent.
 WAM_DEV int mx_encode8(const float* f, u32x2& codes) {
   float amax = 0.f;

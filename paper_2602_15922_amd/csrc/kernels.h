@@ -274,4 +274,53 @@ hipError_t launch_loop_decide(int32_t* state, const float* cs, float tau, int32_
                               int32_t i, hipStream_t s);
 hipError_t launch_copy_if(const int32_t* flag, const float* src, float* dst, int64_t n, hipStream_t s);
 
+// ---- the KV cache in pages (wam_paged_cache and the entry points around it) ----
+// n / d for 0 <= n < 2^31 without a division: (n * mul) >> (32 + shift), exact for 1 <= d < 2^31
+// (mul = ceil(2^(31+b) / d) with b = ceil(log2 d), shift = b - 1; the error n * (mul d - 2^(31+b)) / d
+// stays below 2^(31+b) / d since n < 2^31 and mul d - 2^(31+b) < d <= 2^b).
+struct FastDiv {
+  uint32_t d, mul, shift;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t b = 0;
+  while ((1ull << b) < d) ++b;
+  if (d == 1) return FastDiv{1, 0, 0};
+  return FastDiv{d, (uint32_t)(((1ull << (31 + b)) + d - 1) / d), b - 1};
+}
+
+struct PagePlanArgs {
+  wam_page_plan_desc d;
+  FastDiv ps;
+  const int32_t *cache_len, *new_len, *held, *n_free;
+  int32_t *table, *free_list, *held_out, *n_free_out, *q_start, *kv_len, *slots, *token_pos, *status;
+};
+hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s);
+
+struct RopePagedArgs {
+  wam_paged_cache c;
+  FastDiv ps;
+  int32_t T, Hq, n_axes, n, halves;  // n: rotated pairs
+  int64_t qkv_ts, q_ts;
+  const void* qkv;
+  const int32_t *pos, *slots;
+  void* q_out;
+  float v_inv;
+  double turns[64];   // revolutions per position of each pair
+  uint8_t axis[64];
+};
+hipError_t launch_rope_paged(const RopePagedArgs& a, hipStream_t s);
+
+// Ragged attention over pages (table set) or over rows of packed states (table NULL).
+struct RaggedArgs {
+  const void *q, *k, *v, *k_exp;
+  void* o;
+  const int32_t *table, *q_start, *q_len, *k_start, *k_len;  // k_len: kv_len of the paged form
+  int64_t table_stride, q_ts, o_ts;
+  int64_t page_stride, tok_stride, head_stride;
+  int32_t R, T, Hq, Hkv, Dh, max_k, chunk, n_pages, S;
+  FastDiv ps;
+  float c, v_scale;  // c: softmax scale * log2(e)
+};
+hipError_t launch_attn_ragged(const RaggedArgs& a, void* ws, hipStream_t s);
+
 }  // namespace wam
