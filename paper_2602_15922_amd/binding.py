@@ -515,7 +515,7 @@ def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, w
     tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
     T, Hq, _ = q.shape
     R, width = block_table.shape
-    d = wam_attn_paged_desc(R, T, Hq, width, width * cache.page_size if max_kv is None else max_kv, chunk,
+    d = wam_attn_paged_desc(R, T, Hq, width, min(width * cache.page_size, 1 << 30) if max_kv is None else max_kv, chunk,
                             block_table.stride(0), q.stride(0), o.stride(0), scale)
     _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), _p(q), _p(block_table), _p(q_start), _p(q_len), _p(kv_len),
                                 _p(o), _p(ws), 0 if ws is None else ws.numel(), _stream(stream)))

@@ -1,121 +1,686 @@
-// Attention of ragged rows over a paged KV cache, or over packed states of other lengths.
-#include "common.h"
+// Attention of ragged rows over a paged KV cache, or over packed states of other lengths (bf16
+// MFMA, fp32 online softmax).
+//
+// The rows of a request and KV head are its tokens times the query heads that share the KV head,
+// token by token; a workgroup owns 128 of them, so a shared head's keys are read once for its
+// whole group.  Row tile x of the launch belongs to the last request r with floor(q_start[r] G / 128)
+// + r <= x: every request has room for its tiles there, the launch needs only T, G and R, and a
+// workgroup finds its request with one pass over q_start.
+//
+// Two paths by the request's rows:
+//  stream  at most 32 rows (single tokens): bound by reading the cache.  Each wavefront takes every
+//          fourth 32-key tile on its own, K from memory straight into the matrix operand's registers,
+//          V through a private piece of LDS for its transposition; the next tile's 16 KB are in
+//          flight while one is used, nothing waits for another wavefront until the four states are
+//          joined at the end.
+//  tile    more rows: 32 per wavefront against 64-key tiles shared in LDS, as in attn.hip (whose tile
+//          code it shares); the page of a wavefront's 16 keys of a tile is one entry of the
+//          block table (a page holds a multiple of 16 keys).
+// Where rows are few and keys many the key axis is split over workgroups (ragged_plan.h); the parts
+// are joined in a fixed order by ragged_join_kernel.
+#include "attn_tile.h"
 #include "kernels.h"
+#include "ragged_plan.h"
 
 namespace wam {
 namespace {
+
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+struct Parts {
+  float* ml;  // [row][splits][2]: reference and sum
+  float* o;   // [row][splits][Dh]
+  int splits, split_keys, tiles, by_xcd;
+};
 
 WAM_DEV int fdiv(const FastDiv& f, int n) {
   return f.d == 1 ? n : (int)(__umulhi((uint32_t)n, f.mul) >> f.shift);
 }
 WAM_DEV int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+WAM_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// One decoded value of a K or V row.
-template <bool FP8>
-WAM_DEV float value(const void* p, int64_t at) {
-  if constexpr (FP8)
-    return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(p)[at], 0);
-  else
-    return (float)static_cast<const bf16*>(p)[at];
+// A request's rows and keys, cut to what the call names.
+struct Req {
+  int q0, n;       // first token row, tokens
+  int kv, keys;    // length that positions count from; keys there are (at most max_k)
+  int64_t k0;      // packed states: first key row
+};
+template <bool PAGED>
+WAM_DEV Req request(const RaggedArgs& a, int r) {
+  Req q;
+  q.q0 = a.q_start[r];
+  const int end = clampi(a.q_start[r + 1], 0, a.T);
+  q.n = q.q0 < 0 || q.q0 >= end ? 0 : end - q.q0;
+  if (a.q_len) q.n = clampi(a.q_len[r], 0, q.n);
+  if (PAGED) {
+    q.k0 = 0;
+    q.kv = a.k_len[r];
+    q.keys = clampi(q.kv, 0, a.max_k);
+  } else {
+    const int k0 = clampi(a.k_start[r], 0, a.S);
+    const int64_t len = a.k_len ? a.k_len[r] : (int64_t)a.k_start[r + 1] - k0;
+    const int room = a.S - k0 < a.max_k ? a.S - k0 : a.max_k;
+    q.k0 = k0;
+    q.kv = q.keys = len < 0 ? 0 : (len < room ? (int)len : room);
+  }
+  return q;
+}
+// keys that token i of the request sees (a prefix)
+template <bool PAGED>
+WAM_DEV int kend_of(const RaggedArgs& a, const Req& q, int i) {
+  if (!PAGED || a.chunk == 0) return q.keys;
+  const int64_t p = (int64_t)q.kv - q.n + i;
+  if (p < 0) return 0;
+  const int64_t e = (int64_t)((uint32_t)p / (uint32_t)a.chunk + 1) * a.chunk;
+  return e < q.keys ? (int)e : q.keys;
 }
 
-// One wavefront per (token, query head), 64 keys at a time: a lane forms the score of a key, the
-// wavefront keeps the running maximum and sum, and a lane sums the output dims it owns.
+// page of the 16 keys from `key` on (a multiple of 16), -1 where there is none
+template <bool PAGED>
+WAM_DEV int page_of(const RaggedArgs& a, int r, int key, int end) {
+  if (key >= end) return -1;
+  if (!PAGED) return 0;
+  const int p = a.table[r * a.table_stride + fdiv(a.ps, key)];
+  return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+}
+// element offset of the row of `key` in page `page`
+template <bool PAGED>
+WAM_DEV int64_t row_at(const RaggedArgs& a, const Req& q, int page, int key, int hk) {
+  if (!PAGED) return (q.k0 + key) * a.tok_stride + hk * a.head_stride;
+  const int in = key - fdiv(a.ps, key) * (int)a.ps.d;
+  return (int64_t)page * a.page_stride + (int64_t)in * a.tok_stride + hk * a.head_stride;
+}
+
+// 8 E4M3 codes times the power of two sc, exactly, as bf16
+WAM_DEV bf16x8 decode8(uint32_t lo, uint32_t hi, float sc) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+WAM_DEV float exp_scale(uint32_t biased) { return __uint_as_float(biased << 23); }
+
+// ---------------------------------------------------------------------------------
+// stream path
+// ---------------------------------------------------------------------------------
+// 16x16x32 bf16 MFMA.  Lane l, g = l / 16: A[m = l % 16][8 k's of group g], B[8 k's of group g][n =
+// l % 16], D register r: D[m = 4 g + r][n = l % 16]; both operands' k order is free as long as it is one.
+WAM_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// V rows of a tile in a wavefront's LDS: 16-byte chunks XOR-swizzled so that the 8 rows x 32 bytes that 32
+// lanes of the transposing read touch lie in different banks.
+template <int DH>
+WAM_DEV int sswz(int row, int ch) { return DH == 128 ? (ch ^ (2 * (row & 7))) : (ch ^ (2 * ((row >> 1) & 3))); }
+
+// One 32-key tile of a wavefront in registers: two groups of 16 keys.
+template <int DH, bool FP8>
+struct StreamRegs {
+  static constexpr int KN = FP8 ? 2 : DH / 32, VN = FP8 ? 2 : DH / 32;
+  u32x4v k[2][KN], v[2][VN];
+  uint32_t ex[2];
+  int nv[2];  // keys there are of each group (wave-uniform)
+};
+
 template <int DH, bool PAGED, bool FP8>
-__global__ __launch_bounds__(64) void attn_ragged_kernel(const RaggedArgs a) {
-  __shared__ float qs[DH], ps[64];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  // the request of row t: the last whose start is not past it
+WAM_DEV void stream_load(StreamRegs<DH, FP8>& x, const RaggedArgs& a, const Req& q, int hk, int key0, int end, int pg0,
+                         int pg1, int lane) {
+  constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;  // chunks per row, rows per instruction
+  const int g = lane >> 4, n16 = lane & 15;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int key = key0 + 16 * u, pg = u ? pg1 : pg0;
+    const int nv = pg < 0 ? 0 : clampi(end - key, 0, 16);
+    x.nv[u] = nv;
+    if (nv == 0) {
+#pragma unroll
+      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i) x.k[u][i] = x.v[u][i] = u32x4v{0, 0, 0, 0};
+      x.ex[u] = 0;
+      continue;
+    }
+    const int64_t at = row_at<PAGED>(a, q, pg, key, hk);
+    const char* kp = static_cast<const char*>(a.k) + at * EB;
+    const char* vp = static_cast<const char*>(a.v) + at * EB;
+    const int ts = (int)a.tok_stride * EB;
+    // rows past the last key re-read it (their scores are masked, their values zeroed)
+    const int kr = (n16 < nv ? n16 : nv - 1) * ts;
+#pragma unroll
+    for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
+      x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + kr + (FP8 ? 32 * g + 16 * i : 64 * i + 16 * g));
+    if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(a.k_exp) + at / 32 + kr / 32);
+#pragma unroll
+    for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
+      const int row = RPI * i + lane / CPR, rc = row < nv ? row : nv - 1;
+      x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + rc * ts + 16 * (lane % CPR));
+    }
+  }
+}
+
+template <int DH, bool FP8>
+WAM_DEV void stream_store_v(const StreamRegs<DH, FP8>& x, char* vs, int lane) {
+  constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
+      const int row = RPI * i + lane / CPR, ch = lane % CPR;
+      u32x4v v = x.v[u][i];
+      if (x.nv[u] < 16 && row >= x.nv[u]) v = u32x4v{0, 0, 0, 0};
+      char* dst = vs + (16 * u + row) * DH * 2;
+      if constexpr (FP8) {
+        *reinterpret_cast<bf16x8*>(dst + 16 * sswz<DH>(row, 2 * ch)) = decode8(v[0], v[1], 1.0f);
+        *reinterpret_cast<bf16x8*>(dst + 16 * sswz<DH>(row, 2 * ch + 1)) = decode8(v[2], v[3], 1.0f);
+      } else {
+        *reinterpret_cast<u32x4v*>(dst + 16 * sswz<DH>(row, ch)) = v;
+      }
+    }
+}
+
+template <int DH, bool PAGED, bool FP8, int NQ>
+WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int split, bool whole,
+                         int start, int end, char* smem) {
+  constexpr int KS = DH / 32, DT = DH / 16;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, n16 = lane & 15;
+  const int rows = q.n * G;
+  bf16x8 qf[NQ][KS];
+  int row_kend[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int row = 16 * i + n16 < rows ? 16 * i + n16 : rows - 1, tok = row / G;
+    const bf16* qp = static_cast<const bf16*>(a.q) + (q.q0 + tok) * a.q_ts + (hk * G + row - tok * G) * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[i][ks] = load_bf16x8(qp + (FP8 ? 32 * g + 8 * ks : 32 * ks + 8 * g));
+    row_kend[i] = kend_of<PAGED>(a, q, tok);
+  }
+  const int kmin = kend_of<PAGED>(a, q, 0);
+  f32x4 acc[NQ][DT];
+  float m_ref[NQ], l_part[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    m_ref[i] = -INFINITY;
+    l_part[i] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  char* vs = smem + w * 32 * DH * 2;
+  const int j16 = n16;  // transposing read: row 4 g + j/4, 4 dims from 4 (j % 4) of each 16
+  const int vrow = 4 * g + (j16 >> 2);
+  const float c = a.c, thr = RESCALE_LOG2 / c;
+
+  // tile i of this wavefront: keys start + 128 i + 32 w; lane l holds the page of group l % 2 of tile
+  // base + l / 2, for 32 tiles at a time
+  const int first = start + 32 * w;
+  const int n_tiles = end > first ? (end - first + 127) / 128 : 0;
+  int meta = -1;
+  auto pages = [&](int base) { meta = page_of<PAGED>(a, r, first + 128 * (base + (lane >> 1)) + 16 * (lane & 1), end); };
+  StreamRegs<DH, FP8> x;
+  auto load = [&](int i) {
+    if ((i & 31) == 0) pages(i);
+    const int at = 2 * (i & 31);
+    stream_load<DH, PAGED, FP8>(x, a, q, hk, first + 128 * i, end, __builtin_amdgcn_readlane(meta, at),
+                                __builtin_amdgcn_readlane(meta, at + 1), lane);
+  };
+  if (n_tiles > 0) load(0);
+  for (int i = 0; i < n_tiles; ++i) {
+    const int key0 = first + 128 * i;
+    asm volatile("" ::: "memory");  // the reads below are other lanes' rows: no store moves across them (a
+    stream_store_v<DH, FP8>(x, vs, lane);  // wavefront's LDS operations run in order, so nothing waits)
+    asm volatile("" ::: "memory");
+    f32x4 s[NQ][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float sc = FP8 ? exp_scale((x.ex[u] >> (8 * g)) & 255) : 1.f;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf;
+        if constexpr (FP8) {
+          const u32x4v kk = x.k[u][ks >> 1];
+          kf = decode8(kk[2 * (ks & 1)], kk[2 * (ks & 1) + 1], sc);
+        } else {
+          kf = __builtin_bit_cast(bf16x8, x.k[u][ks]);
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) s[n][u] = mfma16(kf, qf[n][ks], s[n][u]);
+      }
+    }
+    const int nv0 = x.nv[0], nv1 = x.nv[1];
+    if (i + 1 < n_tiles) load(i + 1);
+    if (nv0 < 16 || nv1 < 16 || key0 + 32 > kmin) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int kk = 4 * g + e;
+            if (kk >= (u ? nv1 : nv0) || key0 + 16 * u + kk >= row_kend[n]) s[n][u][e] = -INFINITY;
+          }
+    }
+    bf16x8 pb[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float mx = s[n][0][0];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][u][e]);
+      if (__any(mx > m_ref[n] + thr || (m_ref[n] == -INFINITY && mx != -INFINITY))) {
+        // the four lanes of a query raise their common reference together
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool raise = mx > m_ref[n] + thr || (m_ref[n] == -INFINITY && mx != -INFINITY);
+        const float m_new = raise ? mx : m_ref[n];
+        const float alpha = m_ref[n] == -INFINITY ? 0.f : exp2_fast((m_ref[n] - m_new) * c);
+        m_ref[n] = m_new;
+        l_part[n] *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[n][d] *= alpha;
+      }
+      const float ms = m_ref[n] == -INFINITY ? 0.f : m_ref[n] * c;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pb[n][4 * u + e] = (bf16)exp2_fast(__builtin_fmaf(s[n][u][e], c, -ms));
+      // the sum of exactly the bf16 probabilities the value product uses
+      const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        l_part[n] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[n][2 * e], pb[n][2 * e + 1]}, ones, l_part[n], false);
+    }
+    // k slots of the value product: the four keys 4 g .. of group 0, then of group 1, on both sides
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const int ch = 2 * d + ((j16 & 3) >> 1);
+      const char* at = vs + vrow * DH * 2 + 16 * sswz<DH>(vrow, ch) + 8 * (j16 & 1);
+      const s16x4 v2[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at),
+                           __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * DH * 2))};
+      const bf16x8 vf = *reinterpret_cast<const bf16x8*>(v2);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) acc[n][d] = mfma16(vf, pb[n], acc[n][d]);
+    }
+  }
+
+  // join the four wavefronts: common reference, scaled sums, 16 rows at a time through LDS
+  constexpr int PITCH = DH + 4;
+  float* red = reinterpret_cast<float*>(smem);                // [4][16][PITCH]
+  float* wml = red + 4 * 16 * PITCH;                          // [4][16][2]
+  static_assert((4 * 16 * PITCH + 128) * 4 <= 4 * BN * DH * 2, "fits the tiles' LDS");
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float l = l_part[n];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __syncthreads();  // the V tiles (the rows before) are no longer read
+    if (g == 0) {
+      wml[(w * 16 + n16) * 2] = m_ref[n];
+      wml[(w * 16 + n16) * 2 + 1] = l;
+    }
+    __syncthreads();
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, wml[(k * 16 + n16) * 2]);
+    const float f = m_ref[n] == -INFINITY ? 0.f : exp2_fast((m_ref[n] - top) * c);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      *reinterpret_cast<f32x4*>(red + (w * 16 + n16) * PITCH + 16 * d + 4 * g) = acc[n][d] * f;
+    __syncthreads();
+    // thread: row tid / 16, DH / 16 dims
+    constexpr int PER = DH / 16;
+    const int rr = tid >> 4, d0 = (tid & 15) * PER, row = 16 * n + rr;
+    top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, wml[(k * 16 + rr) * 2]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float mk = wml[(k * 16 + rr) * 2];
+      sum += mk == -INFINITY ? 0.f : wml[(k * 16 + rr) * 2 + 1] * exp2_fast((mk - top) * c);
+    }
+    float y[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) y[e] += red[(k * 16 + rr) * PITCH + d0 + e];
+    if (row < rows) {
+      const int tok = row / G, h = hk * G + row - tok * G;
+      if (whole) {
+        const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
+        bf16* op = static_cast<bf16*>(a.o) + (q.q0 + tok) * a.o_ts + h * DH + d0;
+#pragma unroll
+        for (int e = 0; e < PER; e += 4)
+          *reinterpret_cast<bf16x4*>(op + e) =
+              bf16x4{(bf16)(y[e] * inv), (bf16)(y[e + 1] * inv), (bf16)(y[e + 2] * inv), (bf16)(y[e + 3] * inv)};
+      } else {
+        const int64_t id = ((int64_t)(q.q0 + tok) * a.Hq + h) * pt.splits + split;
+        if ((tid & 15) == 0) {
+          pt.ml[2 * id] = top;
+          pt.ml[2 * id + 1] = sum;
+        }
+#pragma unroll
+        for (int e = 0; e < PER; e += 4)
+          *reinterpret_cast<f32x4*>(pt.o + id * DH + d0 + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// tile path
+// ---------------------------------------------------------------------------------
+// What a wavefront needs to fetch its 16 rows (16 w .. 16 w + 15) of a 64-key tile.
+template <int DH, bool PAGED, bool FP8>
+struct Fetch {
+  static constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, N = 16 * CPR / 64;  // 16-byte chunks per lane
+  int koff[N], voff[N], row[N];
+  u32x4v kr[FP8 ? N : 1], vr[FP8 ? N : 1];  // FP8: the tile's codes on their way to LDS
+  uint32_t ex[FP8 ? N : 1];
+
+  WAM_DEV void init(const RaggedArgs& a, int lane) {
+    const int ts = (int)a.tok_stride * EB;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * 64 + lane, rw = u / CPR, ch = u % CPR;
+      row[i] = rw;
+      // (16 w does not change either swizzle)
+      koff[i] = rw * ts + (FP8 ? ch : kswz<DH>(rw, ch)) * 16;
+      voff[i] = rw * ts + (FP8 ? ch : vswz<DH>(rw, ch)) * 16;
+    }
+  }
+  // bf16: into LDS; rows from nv on as zeros.  FP8: into registers.
+  WAM_DEV void load(const RaggedArgs& a, const Req& q, bf16* tile, int key, int pg, int nv, int hk, int w, int lane) {
+    bf16* Ks = tile + 16 * w * DH;
+    bf16* Vs = Ks + BN * DH;
+    const int64_t at = nv > 0 ? row_at<PAGED>(a, q, pg, key, hk) * EB : 0;
+    char* kp = const_cast<char*>(static_cast<const char*>(a.k)) + at;
+    char* vp = const_cast<char*>(static_cast<const char*>(a.v)) + at;
+    if constexpr (FP8) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        kr[i] = vr[i] = u32x4v{0, 0, 0, 0};
+        ex[i] = 0;
+        if (row[i] < nv) {
+          kr[i] = *reinterpret_cast<const u32x4v*>(kp + koff[i]);
+          vr[i] = *reinterpret_cast<const u32x4v*>(vp + voff[i]);
+          ex[i] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(a.k_exp) + at / 32 + (koff[i] & ~127) / 32);
+        }
+      }
+    } else if (nv == 16) {
+      const __amdgpu_buffer_rsrc_t kres = __builtin_amdgcn_make_buffer_rsrc(kp, (short)0, 0x7fffffff, 0x00020000);
+      const __amdgpu_buffer_rsrc_t vres = __builtin_amdgcn_make_buffer_rsrc(vp, (short)0, 0x7fffffff, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kres, (lds_void*)(Ks + i * 512), 16, koff[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vres, (lds_void*)(Vs + i * 512), 16, voff[i], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        u32x4v kk = {0, 0, 0, 0}, vv = {0, 0, 0, 0};
+        if (row[i] < nv) {
+          kk = *reinterpret_cast<const u32x4v*>(kp + koff[i]);
+          vv = *reinterpret_cast<const u32x4v*>(vp + voff[i]);
+        }
+        *reinterpret_cast<u32x4v*>(Ks + i * 512 + lane * 8) = kk;
+        *reinterpret_cast<u32x4v*>(Vs + i * 512 + lane * 8) = vv;
+      }
+    }
+  }
+  // FP8: the codes decoded into LDS (chunk ch of 16 dims: two 16-byte chunks of bf16)
+  WAM_DEV void store(bf16* tile, int w, int lane) {
+    if constexpr (FP8) {
+      bf16* Ks = tile + 16 * w * DH;
+      bf16* Vs = Ks + BN * DH;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int ch = (i * 64 + lane) % CPR;
+        const float sc = exp_scale((ex[i] >> (8 * (ch >> 1))) & 255);
+        bf16 *kd = Ks + row[i] * DH, *vd = Vs + row[i] * DH;
+        *reinterpret_cast<bf16x8*>(kd + 8 * kswz<DH>(row[i], 2 * ch)) = decode8(kr[i][0], kr[i][1], sc);
+        *reinterpret_cast<bf16x8*>(kd + 8 * kswz<DH>(row[i], 2 * ch + 1)) = decode8(kr[i][2], kr[i][3], sc);
+        *reinterpret_cast<bf16x8*>(vd + 8 * vswz<DH>(row[i], 2 * ch)) = decode8(vr[i][0], vr[i][1], 1.0f);
+        *reinterpret_cast<bf16x8*>(vd + 8 * vswz<DH>(row[i], 2 * ch + 1)) = decode8(vr[i][2], vr[i][3], 1.0f);
+      }
+    }
+  }
+};
+
+// scores, mask (row_kend: the lane's prefix; groups: which of the tile's four 16-key groups have a page), softmax,
+// value product
+template <int DH, bool MASK>
+WAM_DEV void ragged_tile(const char* Ks, const bf16x8* qf, f32x16* acc, float& m_ref, float& l_part, const int* kofs,
+                         const int* vofs, float c, float thr, int kb, int row_kend, int groups, int hh) {
+  f32x16 s[2] = {f32x16{}, f32x16{}};
+  __builtin_amdgcn_s_setprio(1);
+  scores_tile<DH>(Ks, kofs, qf, s);
+  __builtin_amdgcn_s_setprio(0);
+  if (MASK) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = kb + 32 * nt + 8 * (r >> 2) + 4 * hh + (r & 3);
+        if (key >= row_kend || !((groups >> (2 * nt + (r >> 3))) & 1)) s[nt][r] = -INFINITY;
+      }
+  }
+  softmax_pv<DH>(s, Ks + BN * DH * 2, acc, m_ref, l_part, vofs, c, thr);
+}
+
+template <int DH, bool PAGED, bool FP8>
+WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
+                       bool whole, int start, int end, bf16* smem) {
+  constexpr int KS = DH / 16, MT = DH / 32, TILE = 2 * BN * DH;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), hh = lane >> 5, l32 = lane & 31;
+  const int rows = q.n * G;
+  const int qrow = m0 + 32 * w + l32, qc = qrow < rows ? qrow : rows - 1, tok = qc / G, head = hk * G + qc - tok * G;
+  const int row_kend = kend_of<PAGED>(a, q, tok);
+  const int kmin = kend_of<PAGED>(a, q, m0 / G);
+  bf16x8 qf[KS];
+  {
+    const bf16* qp = static_cast<const bf16*>(a.q) + (q.q0 + tok) * a.q_ts + head * DH + 8 * hh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = load_bf16x8(qp + 16 * ks);
+  }
+  // LDS operand offsets, as in attn.hip
+  int kofs[KS], vofs[MT];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) kofs[ks] = l32 * DH * 2 + kswz<DH>(l32, 2 * ks + hh) * 16;
+  {
+    const int grp = lane >> 4, j16 = lane & 15, r0 = 4 * (grp >> 1) + (j16 >> 2);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int col = 32 * mt + 16 * (grp & 1) + 4 * (j16 & 3);
+      vofs[mt] = r0 * DH * 2 + vswz<DH>(r0, col >> 3) * 16 + 8 * ((col >> 2) & 1);
+    }
+  }
+  f32x16 acc[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x16{};
+  float m_ref = -INFINITY, l_part = 0.f;
+  const float c = a.c, thr = RESCALE_LOG2 / c;
+
+  const int t0 = start / BN, nt = end > start ? (end + BN - 1) / BN : t0;
+  const int n_plain = kmin / BN;  // tiles before it hide no key from any row
+  Fetch<DH, PAGED, FP8> f;
+  f.init(a, lane);
+  // pages of a window of 16 tiles, lane l: keys 16 l .. of it; and of the next window
+  int meta = page_of<PAGED>(a, r, start + 16 * lane, end), meta_next = -1;
+  auto fetch = [&](int t, int wend) {
+    const int key = t * BN + 16 * w, pg = __builtin_amdgcn_readlane(t < wend ? meta : meta_next, (4 * (t - t0) + w) & 63);
+    const int nv = pg < 0 ? 0 : clampi(end - key, 0, 16);
+    f.load(a, q, smem + ((t - t0) & 1) * TILE, key, pg, nv, hk, w, lane);
+  };
+  if (nt > t0) {
+    fetch(t0, t0 + 16);
+    f.store(smem, w, lane);
+  }
+  tile_sync();
+  for (int wb = t0; wb < nt; wb += 16) {
+    const int we = wb + 16 < nt ? wb + 16 : nt;
+    meta_next = page_of<PAGED>(a, r, (wb + 16) * BN + 16 * lane, end);
+    // (groups past the end count as present: the rows' prefixes hide them)
+    const uint64_t there = __ballot(meta >= 0 || wb * BN + 16 * lane >= end);
+    const int plain = ~there == 0 ? (n_plain < we ? n_plain : we) : wb;
+    int t = wb;
+    auto step = [&](int cur, auto mask) {
+      if (t + 1 < nt) fetch(t + 1, wb + 16);
+      const char* Ks = reinterpret_cast<const char*>(smem + cur * TILE);
+      ragged_tile<DH, decltype(mask)::value>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend,
+                                             (int)(there >> (4 * (t - wb))) & 15, hh);
+      if (t + 1 < nt) f.store(smem + (cur ^ 1) * TILE, w, lane);
+      tile_sync();
+      ++t;
+    };
+    while (t + 2 <= plain) {
+      step(0, std::false_type{});
+      step(1, std::false_type{});
+    }
+    while (t < we) step((t - t0) & 1, std::true_type{});
+    meta = meta_next;
+  }
+
+  const float l = l_part + other_half(l_part);
+  if (qrow >= rows) return;
+  if (whole) {
+    const float inv = l > 0.f ? (FP8 ? a.v_scale : 1.f) / l : 0.f;
+    bf16* ob = static_cast<bf16*>(a.o) + (q.q0 + tok) * a.o_ts + head * DH;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        *reinterpret_cast<bf16x4*>(ob + 32 * mt + 8 * rr + 4 * hh) =
+            bf16x4{(bf16)(acc[mt][4 * rr + 0] * inv), (bf16)(acc[mt][4 * rr + 1] * inv),
+                   (bf16)(acc[mt][4 * rr + 2] * inv), (bf16)(acc[mt][4 * rr + 3] * inv)};
+  } else {
+    const int64_t id = ((int64_t)(q.q0 + tok) * a.Hq + head) * pt.splits + split;
+    if (hh == 0) {
+      pt.ml[2 * id] = m_ref;
+      pt.ml[2 * id + 1] = l;
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        *reinterpret_cast<f32x4*>(pt.o + id * DH + 32 * mt + 8 * rr + 4 * hh) =
+            f32x4{acc[mt][4 * rr + 0], acc[mt][4 * rr + 1], acc[mt][4 * rr + 2], acc[mt][4 * rr + 3]};
+  }
+}
+
+// last request whose start (in units of 1 / scale rows, plus its number where by_tile) is not past x, or -1
+WAM_DEV int find_request(const RaggedArgs& a, int x, int G, bool by_tile, int lane) {
   int cnt = 0;
   for (int b = 0; b < a.R; b += 64) {
-    const bool in = b + lane < a.R && a.q_start[b + lane] <= t;
+    const int r = b + lane;
+    bool in = false;
+    if (r < a.R) in = by_tile ? (((int64_t)a.q_start[r] * G) >> 7) + r <= x : a.q_start[r] <= x;
     cnt += __popcll(__ballot(in));
   }
-  const int r = cnt - 1;
-  if (r < 0) return;
-  const int q0 = a.q_start[r], room = clampi(a.q_start[r + 1], 0, a.T) - q0;
-  int n = a.q_len ? a.q_len[r] : room;
-  n = n < room ? n : room;
-  if (q0 < 0 || t - q0 >= n) return;
-  int64_t k0 = 0;
-  int kv, kend;
-  if (PAGED) {
-    kv = a.k_len[r];
-    kend = kv;
-    const int64_t p = (int64_t)kv - n + (t - q0);
-    if (a.chunk) {
-      const int64_t e = p < 0 ? 0 : (p / a.chunk + 1) * a.chunk;
-      kend = e < kend ? (int)e : kend;
-    }
+  return cnt - 1;
+}
+static_assert(RAGGED_ROWS == 128, "the shift above");
+
+template <int DH, bool PAGED, bool FP8>
+__global__ __launch_bounds__(NT, 2) void attn_ragged_kernel(const RaggedArgs a, const Parts pt) {
+  __shared__ __attribute__((aligned(16))) bf16 smem[4 * BN * DH];
+  const int G = a.Hq / a.Hkv, lane = threadIdx.x & 63;
+  int x, hk, split;
+  if (pt.by_xcd) {
+    // rows share keys with their neighbours: each XCD a contiguous range of (row tile, head) pairs
+    const int nblk = gridDim.x, bi = blockIdx.x, xcd = bi & 7, per = nblk >> 3, rem = nblk & 7;
+    const int lid = xcd * per + (xcd < rem ? xcd : rem) + (bi >> 3);
+    x = lid % pt.tiles;
+    hk = lid / pt.tiles % a.Hkv;
+    split = lid / pt.tiles / a.Hkv;
   } else {
-    k0 = clampi(a.k_start[r], 0, a.S);
-    kend = a.k_len ? a.k_len[r] : a.k_start[r + 1] - (int)k0;
-    kend = kend < a.S - k0 ? kend : a.S - (int)k0;
+    hk = blockIdx.x % a.Hkv;
+    split = blockIdx.x / a.Hkv % pt.splits;
+    x = blockIdx.x / a.Hkv / pt.splits;
   }
-  kend = clampi(kend, 0, a.max_k);
-  const int hk = h / (a.Hq / a.Hkv);
-  for (int i = lane; i < DH; i += 64) qs[i] = (float)(static_cast<const bf16*>(a.q)[t * a.q_ts + h * DH + i]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, acc[DH / 64] = {};
-  for (int kb = 0; kb < kend; kb += 64) {
-    const int j = kb + lane;
-    int64_t at = -1;
-    if (j < kend) {
-      if (PAGED) {
-        const int e = fdiv(a.ps, j), page = a.table[r * a.table_stride + e];
-        if (page >= 0 && page < a.n_pages)
-          at = page * a.page_stride + (int64_t)(j - e * (int)a.ps.d) * a.tok_stride + hk * a.head_stride;
-      } else {
-        at = (k0 + j) * a.tok_stride + hk * DH;
-      }
-    }
-    float s = -INFINITY;
-    if (at >= 0) {
-      s = 0.f;
-      const uint32_t ex = FP8 ? static_cast<const uint32_t*>(a.k_exp)[at / 128] : 0;
-      for (int b = 0; b < DH / 32; ++b) {
-        float part = 0.f;
-        for (int i = 32 * b; i < 32 * b + 32; ++i) part += qs[i] * value<FP8>(a.k, at + i);
-        s += FP8 ? ldexpf(part, (int)((ex >> (8 * b)) & 255) - 127) : part;
-      }
-    }
-    float mx = s;
-    for (int x = 1; x < 64; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
-    const float alpha = exp2_fast((m - ref) * a.c);
-    const float p = exp2_fast((s - ref) * a.c);
-    float sum = p;
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    m = mn;
-    l = l * alpha + sum;
-    ps[lane] = p;
-    __syncthreads();
-    for (int i = 0; i < DH / 64; ++i) acc[i] *= alpha;
-    for (int jj = 0; jj < 64; ++jj) {
-      const int64_t row = __shfl(at, jj, 64);
-      if (row < 0) continue;
-      for (int i = 0; i < DH / 64; ++i) acc[i] += ps[jj] * value<FP8>(a.v, row + lane + 64 * i);
-    }
-    __syncthreads();
+  const int r = uniform(find_request(a, x, G, true, lane));
+  if (r < 0) return;
+  const Req q = request<PAGED>(a, r);
+  const int64_t m0 = ((int64_t)x - r - (((int64_t)q.q0 * G) >> 7)) * RAGGED_ROWS;
+  const int rows = q.n * G;
+  if (m0 < 0 || m0 >= rows) return;
+  const int start = split * pt.split_keys;
+  if (split > 0 && start >= q.keys) return;
+  const bool whole = q.keys <= pt.split_keys;
+  const int last = m0 + RAGGED_ROWS < rows ? (int)m0 + RAGGED_ROWS - 1 : rows - 1;
+  const int kmax = kend_of<PAGED>(a, q, last / G);
+  const int end = kmax - start < pt.split_keys ? kmax : start + pt.split_keys;
+  if (rows > RAGGED_STREAM)
+    tile_rows<DH, PAGED, FP8>(a, pt, q, r, hk, G, (int)m0, split, whole, start, end, smem);
+  else if (rows > 16)
+    stream_rows<DH, PAGED, FP8, 2>(a, pt, q, r, hk, G, split, whole, start, end, reinterpret_cast<char*>(smem));
+  else
+    stream_rows<DH, PAGED, FP8, 1>(a, pt, q, r, hk, G, split, whole, start, end, reinterpret_cast<char*>(smem));
+}
+
+// o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over a row's parts, a wavefront per (token, head)
+template <int DH, bool PAGED, bool FP8>
+__global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, const Parts pt) {
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int t = (int)(id / a.Hq), h = (int)(id - (int64_t)t * a.Hq);
+  if (t >= a.T) return;
+  const int r = find_request(a, t, 1, false, lane);
+  if (r < 0) return;
+  const Req q = request<PAGED>(a, r);
+  if (t - q.q0 >= q.n || q.keys <= pt.split_keys) return;
+  const int n = (q.keys + pt.split_keys - 1) / pt.split_keys;
+  float m = -INFINITY, l = 0.f;
+  if (lane < n) {
+    m = pt.ml[2 * (id * pt.splits + lane)];
+    l = pt.ml[2 * (id * pt.splits + lane) + 1];
   }
-  const float inv = l > 0.f ? (FP8 ? a.v_scale : 1.f) / l : 0.f;
-  for (int i = 0; i < DH / 64; ++i)
-    static_cast<bf16*>(a.o)[t * a.o_ts + h * DH + lane + 64 * i] = (bf16)(acc[i] * inv);
+  float top = m;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
+  const float f = l != 0.f ? exp2_fast((m - top) * a.c) : 0.f;
+  const float sum = wave_sum(f * l);
+  constexpr int PER = DH / 64;
+  float y[PER] = {};
+  for (int s = 0; s < n; ++s) {
+    const float fs = __shfl(f, s, 64);
+    if (fs == 0.f) continue;  // nothing was stored for a part without keys
+#pragma unroll
+    for (int e = 0; e < PER; ++e) y[e] += fs * pt.o[(id * pt.splits + s) * DH + lane * PER + e];
+  }
+  const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
+  bf16* op = static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + lane * PER;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) op[e] = (bf16)(y[e] * inv);
+}
+
+template <int DH, bool PAGED, bool FP8>
+hipError_t launch(const RaggedArgs& a, const Parts& pt, hipStream_t s) {
+  const int64_t grid = (int64_t)pt.tiles * a.Hkv * pt.splits;
+  hipLaunchKernelGGL((attn_ragged_kernel<DH, PAGED, FP8>), dim3((unsigned)grid), dim3(NT), 0, s, a, pt);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || pt.splits == 1) return e;
+  hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8>), dim3((unsigned)(((int64_t)a.T * a.Hq + 3) / 4)), dim3(256), 0,
+                     s, a, pt);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_ragged(const RaggedArgs& a, void*, hipStream_t s) {
-  const dim3 grid((unsigned)a.T, (unsigned)a.Hq), block(64);
+hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws, hipStream_t s) {
+  Parts pt;
+  pt.ml = static_cast<float*>(ws);
+  pt.o = reinterpret_cast<float*>(static_cast<char*>(ws) + ragged_ml_bytes(p, a.T, a.Hq));
+  pt.splits = p.splits;
+  pt.split_keys = p.split_keys;
+  pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv);
+  pt.by_xcd = !p.few;
   if (a.table) {
-    if (a.k_exp) hipLaunchKernelGGL((attn_ragged_kernel<128, true, true>), grid, block, 0, s, a);
-    else if (a.Dh == 128) hipLaunchKernelGGL((attn_ragged_kernel<128, true, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_ragged_kernel<64, true, false>), grid, block, 0, s, a);
-  } else {
-    if (a.Dh == 128) hipLaunchKernelGGL((attn_ragged_kernel<128, false, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_ragged_kernel<64, false, false>), grid, block, 0, s, a);
+    if (a.k_exp) return launch<128, true, true>(a, pt, s);
+    return a.Dh == 128 ? launch<128, true, false>(a, pt, s) : launch<64, true, false>(a, pt, s);
   }
-  return hipGetLastError();
+  return a.Dh == 128 ? launch<128, false, false>(a, pt, s) : launch<64, false, false>(a, pt, s);
 }
 
 }  // namespace wam

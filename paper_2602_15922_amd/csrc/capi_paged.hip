@@ -62,6 +62,9 @@ wam_status check_ragged(int32_t R, int32_t T, int32_t Hq, int32_t Hkv, int32_t D
   TRY(check_heads(Hq, Hkv, Dh));
   CHECK(Hq % Hkv == 0, WAM_EINVAL, "Hq=%d must be a multiple of Hkv=%d", Hq, Hkv);
   CHECK(R >= 0 && T >= 0 && max_k >= 0, WAM_EINVAL, "negative size (R=%d T=%d longest=%d)", R, T, max_k);
+  CHECK(max_k <= 1 << 30, WAM_EUNSUPPORTED, "the longest key axis %d exceeds 2^30", max_k);
+  CHECK((int64_t)T * Hq <= INT32_MAX && ragged_tiles(R, T, Hq, Hkv) * Hkv <= INT32_MAX / RAGGED_MAX_SPLITS,
+        WAM_EUNSUPPORTED, "T * Hq and (R + T * Hq / Hkv / 128) * Hkv * 64 must stay below 2^31");
   return WAM_OK;
 }
 wam_status check_rows(const void* q, const void* o, int64_t q_ts, int64_t o_ts, int64_t hd) {
@@ -171,8 +174,8 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
 }
 
 size_t wam_attn_paged_workspace_bytes(const wam_attn_paged_desc* desc, const wam_paged_cache* cache) {
-  if (!desc || !cache) return 0;
-  return 0;
+  if (!desc || !cache || check_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv) != WAM_OK) return 0;
+  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, desc->max_kv), desc->T, desc->Hq, cache->Dh);
 }
 
 wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache* cache, const void* q,
@@ -192,7 +195,8 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   TRY(opt_ints(q_len, "q_len"));
   TRY(need_ints(kv_len, "kv_len"));
   if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
-  TRY(check_ws(ws, ws_bytes, wam_attn_paged_workspace_bytes(desc, cache)));
+  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, d.max_kv);
+  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
   RaggedArgs a{};
   a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
   // (a table without columns is never read: no key is below max_k = 0; its address only says "paged")
@@ -206,13 +210,13 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   a.ps = fast_div((uint32_t)c.page_size);
   a.c = exp2_scale(d.scale, c.Dh);
   a.v_scale = c.v_scale;
-  HIPCHECK(launch_attn_ragged(a, ws, stream));
+  HIPCHECK(launch_attn_ragged(a, p, ws, stream));
   return WAM_OK;
 }
 
 size_t wam_attn_cross_workspace_bytes(const wam_attn_cross_desc* desc) {
-  if (!desc) return 0;
-  return 0;
+  if (!desc || check_ragged(desc->R, desc->T, desc->Hq, desc->Hkv, desc->Dh, desc->max_k) != WAM_OK) return 0;
+  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, desc->Hkv, desc->max_k), desc->T, desc->Hq, desc->Dh);
 }
 
 wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const void* k, const void* v,
@@ -228,14 +232,15 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
     TRY(need_ptr(k, "k"));
     TRY(need_ptr(v, "v"));
     CHECK(d.kv_tok_stride >= (int64_t)d.Hkv * d.Dh && d.kv_tok_stride % 8 == 0 &&
-              d.kv_tok_stride <= INT64_MAX / 4 / d.S, WAM_EINVAL,
-          "kv_tok_stride must be a multiple of 8, >= Hkv*Dh=%lld", (long long)d.Hkv * d.Dh);
+              d.kv_tok_stride <= 1 << 25, WAM_EINVAL,
+          "kv_tok_stride must be a multiple of 8, >= Hkv*Dh=%lld and at most 2^25", (long long)d.Hkv * d.Dh);
   }
   TRY(need_ints(q_start, "q_start"));
   TRY(opt_ints(q_len, "q_len"));
   TRY(need_ints(k_start, "k_start"));
   TRY(opt_ints(k_len, "k_len"));
-  TRY(check_ws(ws, ws_bytes, wam_attn_cross_workspace_bytes(desc)));
+  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, d.Hkv, d.max_k);
+  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, d.Dh)));
   RaggedArgs a{};
   a.q = q; a.k = k; a.v = v; a.o = o;
   a.q_start = q_start; a.q_len = q_len; a.k_start = k_start; a.k_len = k_len;
@@ -244,7 +249,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   a.max_k = d.max_k < d.S ? d.max_k : d.S;
   a.ps = fast_div(1);
   a.c = exp2_scale(d.scale, d.Dh);
-  HIPCHECK(launch_attn_ragged(a, ws, stream));
+  HIPCHECK(launch_attn_ragged(a, p, ws, stream));
   return WAM_OK;
 }
 

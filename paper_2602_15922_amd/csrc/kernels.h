@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/wamdit.h"
+#include "ragged_plan.h"
 
 namespace wam {
 
@@ -321,6 +322,6 @@ struct RaggedArgs {
   FastDiv ps;
   float c, v_scale;  // c: softmax scale * log2(e)
 };
-hipError_t launch_attn_ragged(const RaggedArgs& a, void* ws, hipStream_t s);
+hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws, hipStream_t s);
 
 }  // namespace wam
