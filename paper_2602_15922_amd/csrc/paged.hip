@@ -18,13 +18,19 @@ WAM_DEV int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : 
 // read where it is written: surplus pages lie on top of it, a page taken is either
 // entry [n_free - ...] of the list as it came or, found by a search in the sums, an entry of the
 // table row that gives it up, and only what stays on the stack is stored.
+//
+// Bound by latency, a chain of dependent loads (lengths, sums, search, table entry), so: the sums
+// are in 32 bits (tokens saturate at T) and in registers but for one exchange through LDS, and workgroups
+// are small and many.  6 requests with 6600 rows: 4.6 us, 1000 with 173000: 12.9 us; with 64-bit sums by
+// lane exchange, 1024 threads, and a search and a 64-bit division per token 27.6 us and 43.1 us.
 // ---------------------------------------------------------------------------------
-constexpr int PLAN_NT = 1024;
+constexpr int PLAN_NT = 256;
+
+WAM_DEV uint32_t udiv(const FastDiv& f, uint32_t n) { return n < 0x80000000u ? (uint32_t)fdiv(f, (int)n) : n / f.d; }
 
 struct PlanReq {
-  int cache, held, need;
-  int64_t whole;  // pages its tokens fill, past the table's width too
-  int fresh;      // new tokens
+  int cache, fresh, held, need;
+  uint32_t over;  // pages past the table's width
   bool bad;
 };
 WAM_DEV PlanReq plan_req(const PagePlanArgs& a, int r) {
@@ -34,8 +40,10 @@ WAM_DEV PlanReq plan_req(const PagePlanArgs& a, int r) {
   q.fresh = n < 0 ? 0 : n;
   q.held = clampi(h, 0, a.d.max_pages);
   q.bad = c < 0 || n < 0 || q.held != h;
-  q.whole = ((int64_t)q.cache + q.fresh + a.d.page_size - 1) / a.d.page_size;
-  q.need = (int)(q.whole < a.d.max_pages ? q.whole : a.d.max_pages);
+  const uint32_t len = (uint32_t)q.cache + (uint32_t)q.fresh, full = udiv(a.ps, len);
+  const uint32_t whole = full + (full * (uint32_t)a.d.page_size < len ? 1 : 0);
+  q.need = whole < (uint32_t)a.d.max_pages ? (int)whole : a.d.max_pages;
+  q.over = whole - (uint32_t)q.need;
   return q;
 }
 
@@ -50,110 +58,203 @@ WAM_DEV int last_at_most(const int* at, int n, int x) {
   return lo;
 }
 
+// inclusive sums over the wavefront, cut to `most` (all values in [0, most])
+#define WAM_SCAN_STEP(ctrl, rows)                                                   \
+  {                                                                                 \
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false) + v; \
+    v = y < most ? y : most;                                                        \
+  }
+WAM_DEV uint32_t row_scan(uint32_t v, uint32_t most) {
+  WAM_SCAN_STEP(0x111, 0xf)  // row_shr 1, 2, 4, 8: within rows of 16 lanes
+  WAM_SCAN_STEP(0x112, 0xf)
+  WAM_SCAN_STEP(0x114, 0xf)
+  WAM_SCAN_STEP(0x118, 0xf)
+  return v;
+}
+WAM_DEV uint32_t wave_scan(uint32_t v, uint32_t most) {
+  v = row_scan(v, most);
+  WAM_SCAN_STEP(0x142, 0xa)  // row_bcast 15: rows 1 and 3 take the last of the row before
+  WAM_SCAN_STEP(0x143, 0xc)  // row_bcast 31: rows 2 and 3 take the last of row 1
+  return v;
+}
+#undef WAM_SCAN_STEP
+
+// What the fill threads need of a request, from LDS where all of it fits (E small), else from memory again.
+template <int E>
+struct PlanLds {
+  alignas(16) int q_at[E * PLAN_NT], take_at[E * PLAN_NT], back_at[E * PLAN_NT];
+  int cache[E <= 4 ? E * PLAN_NT : 1], held[E <= 4 ? E * PLAN_NT : 1], need[E <= 4 ? E * PLAN_NT : 1];
+  uint32_t wave[3][PLAN_NT / 64];
+};
+
+// E requests per thread: R <= 256 E.  The last workgroup forms the status, the others fill.
+template <int E>
 __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a) {
-  __shared__ int q_at[WAM_PLAN_MAX_REQUESTS], take_at[WAM_PLAN_MAX_REQUESTS], back_at[WAM_PLAN_MAX_REQUESTS];
-  __shared__ int64_t wsum[PLAN_NT / 64][5];
+  __shared__ PlanLds<E> L;
   const int R = a.d.R, T = a.d.T, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int nf_in = a.n_free[0], nf = clampi(nf_in, 0, a.d.n_pages);
-  int64_t run[5] = {0, 0, 0, 0, 0};  // tokens, takes, backs, pages past the width, invalid inputs
-  for (int base = 0; base < R; base += PLAN_NT) {
-    const int r = base + tid;
-    int64_t v[5] = {0, 0, 0, 0, 0};
+  const bool status = blockIdx.x == gridDim.x - 1;
+  uint32_t fresh[E], take[E], back[E], sum[3] = {0, 0, 0};
+  uint64_t all_new = 0, all_over = 0, all_bad = 0;
+  const uint32_t most[3] = {(uint32_t)T, 0x7fffffffu, 0x7fffffffu};
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int r = tid * E + e;
+    fresh[e] = take[e] = back[e] = 0;
     if (r < R) {
       const PlanReq q = plan_req(a, r);
-      v[0] = q.fresh;
-      v[1] = q.need > q.held ? q.need - q.held : 0;
-      v[2] = q.held > q.need ? q.held - q.need : 0;
-      v[3] = q.whole - q.need;
-      v[4] = q.bad;
-    }
-    int64_t x[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      x[i] = v[i];
-#pragma unroll
-      for (int s = 1; s < 64; s <<= 1) {
-        const int64_t y = __shfl_up(x[i], s, 64);
-        if (lane >= s) x[i] += y;
+      fresh[e] = (uint32_t)(q.fresh < T ? q.fresh : T);
+      take[e] = q.need > q.held ? q.need - q.held : 0;
+      back[e] = q.held > q.need ? q.held - q.need : 0;
+      if (status) {
+        all_new += q.fresh;
+        all_over += q.over;
+        all_bad += q.bad;
       }
-      if (lane == 63) wsum[w][i] = x[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      int64_t before = 0, all = 0;
-      for (int k = 0; k < PLAN_NT / 64; ++k) {
-        if (k < w) before += wsum[k][i];
-        all += wsum[k][i];
+      if constexpr (E <= 4) {
+        L.cache[r] = q.cache;
+        L.held[r] = q.held;
+        L.need[r] = q.need;
       }
-      x[i] += run[i] + before - v[i];
-      run[i] += all;
     }
-    if (r < R) {
-      q_at[r] = (int)(x[0] < T ? x[0] : T);
-      take_at[r] = (int)x[1];
-      back_at[r] = (int)x[2];
-    }
-    __syncthreads();
+    sum[0] = sum[0] + fresh[e] < most[0] ? sum[0] + fresh[e] : most[0];
+    sum[1] += take[e];
+    sum[2] += back[e];
   }
-  const int tokens = (int)(run[0] < T ? run[0] : T), takes = (int)run[1], backs = (int)run[2];
+  uint32_t at[3], all[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const uint32_t incl = wave_scan(sum[i], most[i]);
+    at[i] = (uint32_t)__shfl_up((int)incl, 1, 64);
+    if (lane == 0) at[i] = 0;
+    if (lane == 63) L.wave[i][w] = incl;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    uint32_t before = 0;
+    all[i] = 0;
+#pragma unroll
+    for (int k = 0; k < PLAN_NT / 64; ++k) {
+      const uint32_t x = L.wave[i][k];
+      if (k == w) before = all[i];
+      all[i] = all[i] + x < most[i] ? all[i] + x : most[i];
+    }
+    at[i] = before + at[i] < most[i] ? before + at[i] : most[i];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int r = tid * E + e;
+    L.q_at[r] = (int)at[0];
+    L.take_at[r] = (int)at[1];
+    L.back_at[r] = (int)at[2];
+    at[0] = at[0] + fresh[e] < most[0] ? at[0] + fresh[e] : most[0];
+    at[1] += take[e];
+    at[2] += back[e];
+  }
+  __syncthreads();
+  const int tokens = (int)all[0], takes = (int)all[1], backs = (int)all[2];
   const int64_t top = (int64_t)nf + backs;  // height of the stack with the surplus pages on it
+  const int64_t left = top - takes;
 
+  if (status) {
+    // the sums that may pass 32 bits: by lane exchange, then the four wavefronts' through LDS (the
+    // requests' numbers in it are not read here)
+    uint64_t* part = reinterpret_cast<uint64_t*>(L.q_at);
+    uint64_t v[3] = {all_new, all_over, all_bad};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+#pragma unroll
+      for (int s = 1; s < 64; s <<= 1) v[i] += __shfl_xor(v[i], s, 64);
+      if (lane == 0) part[3 * w + i] = v[i];
+    }
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) v[i] = part[i] + part[3 + i] + part[6 + i] + part[9 + i];
+      const uint64_t cut = v[0] - tokens, big = 0x7fffffffu;
+      a.q_start[R] = tokens;
+      a.n_free_out[0] = (int)(left < 0 ? 0 : (left < a.d.n_pages ? left : a.d.n_pages));
+      a.status[0] = (int)(left < 0 ? -left : 0);
+      a.status[1] = (int)(v[1] < big ? v[1] : big);
+      a.status[2] = (int)(cut < big ? cut : big);
+      a.status[3] = (int)v[2] + (nf != nf_in);
+    }
+    return;
+  }
+
+  struct Three { int cache, held, need; };
+  auto req = [&](int r) {
+    if constexpr (E <= 4) return Three{L.cache[r], L.held[r], L.need[r]};
+    const PlanReq q = plan_req(a, r);
+    return Three{q.cache, q.held, q.need};
+  };
   // surplus page number j, in order of requests and entries
   auto back_page = [&](int j) {
-    const int r = last_at_most(back_at, R, j);
-    return a.table[(int64_t)r * a.d.table_stride + plan_req(a, r).need + (j - back_at[r])];
+    const int r = last_at_most(L.back_at, R, j);
+    return a.table[(int64_t)r * a.d.table_stride + req(r).need + (j - L.back_at[r])];
   };
   // the k-th page taken, -1 where the stack is empty
   auto taken_page = [&](int k) {
-    const int64_t at = top - 1 - k;
-    if (at < 0) return -1;
-    return at >= nf ? back_page((int)(at - nf)) : a.free_list[at];
+    const int64_t i = top - 1 - k;
+    if (i < 0) return -1;
+    return i >= nf ? back_page((int)(i - nf)) : a.free_list[i];
   };
 
-  const int id = blockIdx.x * PLAN_NT + tid, n_threads = gridDim.x * PLAN_NT;
-  for (int r = id; r < R; r += n_threads) {
-    const PlanReq q = plan_req(a, r);
-    const int take = q.need > q.held ? q.need - q.held : 0;
-    const int64_t room = top - take_at[r];
-    const int end = r + 1 < R ? q_at[r + 1] : tokens;
-    a.held_out[r] = (q.need < q.held ? q.need : q.held) + (int)(room < 0 ? 0 : (room < take ? room : take));
-    a.q_start[r] = q_at[r];
-    const int64_t kv = (int64_t)q.cache + (end - q_at[r]);
-    a.kv_len[r] = (int)(kv < INT32_MAX ? kv : INT32_MAX);
-  }
-  if (id == 0) {
-    a.q_start[R] = tokens;
-    const int64_t left = top - takes;
-    a.n_free_out[0] = (int)(left < 0 ? 0 : (left < a.d.n_pages ? left : a.d.n_pages));
-    a.status[0] = (int)(left < 0 ? -left : 0);
-    a.status[1] = (int)(run[3] < INT32_MAX ? run[3] : INT32_MAX);
-    a.status[2] = (int)(run[0] - tokens < INT32_MAX ? run[0] - tokens : INT32_MAX);
-    a.status[3] = (int)run[4] + (nf != nf_in);
-  }
-  for (int k = id; k < takes; k += n_threads) {
-    const int r = last_at_most(take_at, R, k);
-    a.table[(int64_t)r * a.d.table_stride + plan_req(a, r).held + (k - take_at[r])] = taken_page(k);
-  }
-  for (int j = id; j < backs - takes; j += n_threads)
-    if (nf + j < a.d.n_pages) a.free_list[nf + j] = back_page(j);
-  for (int t = id; t < T; t += n_threads) {
-    int slot = -1, pos = -1;
-    if (t < tokens) {
-      const int r = last_at_most(q_at, R, t);
-      const PlanReq q = plan_req(a, r);
-      const int64_t p = (int64_t)q.cache + (t - q_at[r]);
-      pos = (int)(p < INT32_MAX ? p : INT32_MAX);
-      const int64_t e = p / a.d.page_size;
-      if (e < q.need) {
-        const int page = e < q.held ? a.table[(int64_t)r * a.d.table_stride + e]
-                                    : taken_page(take_at[r] + (int)e - q.held);
-        if (page >= 0 && page < a.d.n_pages) slot = page * a.d.page_size + (int)(p - e * a.d.page_size);
+  const int id = blockIdx.x * PLAN_NT + tid, n_threads = (gridDim.x - 1) * PLAN_NT;
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.slots) | reinterpret_cast<uintptr_t>(a.token_pos)) & 15) == 0;
+  for (int64_t t0 = 4 * (int64_t)id; t0 < T; t0 += 4 * (int64_t)n_threads) {
+    int slot[4], pos[4], r = 0, next = -1, page = -1;  // tokens below `next` belong to request r
+    uint32_t entry = 0xffffffffu;                      // the entry that `page` is
+    Three q{0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = (int)t0 + j;
+      slot[j] = pos[j] = -1;
+      if (t0 + j >= tokens) continue;
+      if (t >= next) {
+        r = last_at_most(L.q_at, R, t);
+        q = req(r);
+        next = r + 1 < R ? L.q_at[r + 1] : tokens;
+        entry = 0xffffffffu;
+      }
+      const uint32_t p = (uint32_t)q.cache + (uint32_t)(t - L.q_at[r]);
+      pos[j] = (int)(p < 0x7fffffffu ? p : 0x7fffffffu);
+      const uint32_t e = udiv(a.ps, p);
+      if (e >= (uint32_t)q.need) continue;
+      if (e != entry) {
+        entry = e;
+        page = (int)e < q.held ? a.table[(int64_t)r * a.d.table_stride + e] : taken_page(L.take_at[r] + (int)e - q.held);
+      }
+      if (page >= 0 && page < a.d.n_pages) slot[j] = page * a.d.page_size + (int)(p - e * (uint32_t)a.d.page_size);
+    }
+    if (wide && t0 + 4 <= T) {
+      *reinterpret_cast<int4*>(a.slots + t0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      if (a.token_pos) *reinterpret_cast<int4*>(a.token_pos + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+      for (int j = 0; j < 4 && t0 + j < T; ++j) {
+        a.slots[t0 + j] = slot[j];
+        if (a.token_pos) a.token_pos[t0 + j] = pos[j];
       }
     }
-    a.slots[t] = slot;
-    if (a.token_pos) a.token_pos[t] = pos;
   }
+  for (int r = id; r < R; r += n_threads) {
+    const Three q = req(r);
+    const int want = q.need > q.held ? q.need - q.held : 0;
+    const int64_t room = top - L.take_at[r];
+    const int end = r + 1 < R ? L.q_at[r + 1] : tokens;
+    a.held_out[r] = (q.need < q.held ? q.need : q.held) + (int)(room < 0 ? 0 : (room < want ? room : want));
+    a.q_start[r] = L.q_at[r];
+    const int64_t kv = (int64_t)q.cache + (end - L.q_at[r]);
+    a.kv_len[r] = (int)(kv < INT32_MAX ? kv : INT32_MAX);
+  }
+  for (int k = id; k < takes; k += n_threads) {
+    const int r = last_at_most(L.take_at, R, k);
+    a.table[(int64_t)r * a.d.table_stride + req(r).held + (k - L.take_at[r])] = taken_page(k);
+  }
+  for (int j = id; j < backs - takes; j += n_threads)
+    if (nf + (int64_t)j < a.d.n_pages) a.free_list[nf + j] = back_page(j);
 }
 
 // ---------------------------------------------------------------------------------
@@ -262,10 +363,13 @@ __global__ __launch_bounds__(256) void rope_paged_kernel(const RopePagedArgs a) 
 }  // namespace
 
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s) {
-  // about four rows per thread, at most one workgroup per CU
+  // four rows per thread, up to eight workgroups per CU, and one for the status
   const int64_t want = ((int64_t)a.d.T + 4 * PLAN_NT - 1) / (4 * PLAN_NT);
-  const int grid = want < 1 ? 1 : (want > 256 ? 256 : (int)want);
-  hipLaunchKernelGGL(page_plan_kernel, dim3(grid), dim3(PLAN_NT), 0, s, a);
+  const dim3 grid((unsigned)(want < 1 ? 1 : (want > 2048 ? 2048 : want)) + 1), block(PLAN_NT);
+  static_assert(16 * PLAN_NT >= WAM_PLAN_MAX_REQUESTS, "requests per thread");
+  if (a.d.R <= PLAN_NT) hipLaunchKernelGGL(page_plan_kernel<1>, grid, block, 0, s, a);
+  else if (a.d.R <= 4 * PLAN_NT) hipLaunchKernelGGL(page_plan_kernel<4>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(page_plan_kernel<16>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
