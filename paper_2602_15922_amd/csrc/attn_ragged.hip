@@ -31,7 +31,7 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 struct Parts {
   float* ml;  // [row][splits][2]: reference and sum
   float* o;   // [row][splits][Dh]
-  int splits, split_keys, tiles, by_xcd;
+  int splits, split_keys, tiles;
 };
 
 WAM_DEV int fdiv(const FastDiv& f, int n) {
@@ -109,10 +109,9 @@ WAM_DEV float exp_scale(uint32_t biased) { return __uint_as_float(biased << 23);
 // l % 16], D register r: D[m = 4 g + r][n = l % 16]; both operands' k order is free as long as it is one.
 WAM_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// V rows of a tile in a wavefront's LDS: 16-byte chunks XOR-swizzled so that the 8 rows x 32 bytes that 32
-// lanes of the transposing read touch lie in different banks.
-template <int DH>
-WAM_DEV int sswz(int row, int ch) { return DH == 128 ? (ch ^ (2 * (row & 7))) : (ch ^ (2 * ((row >> 1) & 3))); }
+// Bytes between V rows of a tile in a wavefront's LDS: 32 more than a row, so that the 8 rows x 32 bytes that 32 lanes
+// of the transposing read touch lie in different banks, at constant distances.
+constexpr int spitch(int dh) { return dh * 2 + 32; }
 
 // One 32-key tile of a wavefront in registers: two groups of 16 keys.
 template <int DH, bool FP8>
@@ -125,9 +124,9 @@ struct StreamRegs {
 
 template <int DH, bool PAGED, bool FP8>
 WAM_DEV void stream_load(StreamRegs<DH, FP8>& x, const RaggedArgs& a, const Req& q, int hk, int key0, int end, int pg0,
-                         int pg1, int lane) {
+                         int pg1, int lane, int koff, int voff) {
   constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;  // chunks per row, rows per instruction
-  const int g = lane >> 4, n16 = lane & 15;
+  const int ts = (int)a.tok_stride * EB;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int key = key0 + 16 * u, pg = u ? pg1 : pg0;
@@ -142,17 +141,26 @@ WAM_DEV void stream_load(StreamRegs<DH, FP8>& x, const RaggedArgs& a, const Req&
     const int64_t at = row_at<PAGED>(a, q, pg, key, hk);
     const char* kp = static_cast<const char*>(a.k) + at * EB;
     const char* vp = static_cast<const char*>(a.v) + at * EB;
-    const int ts = (int)a.tok_stride * EB;
-    // rows past the last key re-read it (their scores are masked, their values zeroed)
-    const int kr = (n16 < nv ? n16 : nv - 1) * ts;
+    const char* ep = FP8 ? static_cast<const char*>(a.k_exp) + at / 32 : nullptr;
+    if (nv == 16) {  // uniform bases, one lane offset each
 #pragma unroll
-    for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
-      x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + kr + (FP8 ? 32 * g + 16 * i : 64 * i + 16 * g));
-    if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(a.k_exp) + at / 32 + kr / 32);
+      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
+        x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + koff + (FP8 ? 16 : 64) * i);
+      if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep + ((lane & 15) * ts >> 5));
 #pragma unroll
-    for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
-      const int row = RPI * i + lane / CPR, rc = row < nv ? row : nv - 1;
-      x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + rc * ts + 16 * (lane % CPR));
+      for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i)
+        x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + RPI * i * ts + voff);
+    } else {  // rows past the last key re-read it (their scores are masked, their values zeroed)
+      const int n16 = lane & 15, kr = (n16 < nv ? 0 : (nv - 1 - n16) * ts);
+#pragma unroll
+      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
+        x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + koff + kr + (FP8 ? 16 : 64) * i);
+      if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep + ((n16 < nv ? n16 : nv - 1) * ts >> 5));
+#pragma unroll
+      for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
+        const int row = RPI * i + lane / CPR, rc = row < nv ? row : nv - 1;
+        x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + rc * ts + 16 * (lane % CPR));
+      }
     }
   }
 }
@@ -167,19 +175,22 @@ WAM_DEV void stream_store_v(const StreamRegs<DH, FP8>& x, char* vs, int lane) {
       const int row = RPI * i + lane / CPR, ch = lane % CPR;
       u32x4v v = x.v[u][i];
       if (x.nv[u] < 16 && row >= x.nv[u]) v = u32x4v{0, 0, 0, 0};
-      char* dst = vs + (16 * u + row) * DH * 2;
+      char* dst = vs + (16 * u + row) * spitch(DH);
       if constexpr (FP8) {
-        *reinterpret_cast<bf16x8*>(dst + 16 * sswz<DH>(row, 2 * ch)) = decode8(v[0], v[1], 1.0f);
-        *reinterpret_cast<bf16x8*>(dst + 16 * sswz<DH>(row, 2 * ch + 1)) = decode8(v[2], v[3], 1.0f);
+        *reinterpret_cast<bf16x8*>(dst + 32 * ch) = decode8(v[0], v[1], 1.0f);
+        *reinterpret_cast<bf16x8*>(dst + 32 * ch + 16) = decode8(v[2], v[3], 1.0f);
       } else {
-        *reinterpret_cast<u32x4v*>(dst + 16 * sswz<DH>(row, ch)) = v;
+        *reinterpret_cast<u32x4v*>(dst + 16 * ch) = v;
       }
     }
 }
 
+// LDS of the streaming path: four wavefronts' V tiles, or their 16 rows each of the join
+constexpr int stream_lds(int dh) { return (4 * 16 * (dh + 4) + 128) * 4 > 4 * 32 * spitch(dh) ? (4 * 16 * (dh + 4) + 128) * 4 : 4 * 32 * spitch(dh); }
+
 template <int DH, bool PAGED, bool FP8, int NQ>
-WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int split, bool whole,
-                         int start, int end, char* smem) {
+WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
+                         bool whole, int start, int end, char* smem) {
   constexpr int KS = DH / 32, DT = DH / 16;
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, n16 = lane & 15;
   const int rows = q.n * G;
@@ -187,13 +198,13 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
   int row_kend[NQ];
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
-    const int row = 16 * i + n16 < rows ? 16 * i + n16 : rows - 1, tok = row / G;
+    const int row = m0 + 16 * i + n16 < rows ? m0 + 16 * i + n16 : rows - 1, tok = row / G;
     const bf16* qp = static_cast<const bf16*>(a.q) + (q.q0 + tok) * a.q_ts + (hk * G + row - tok * G) * DH;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[i][ks] = load_bf16x8(qp + (FP8 ? 32 * g + 8 * ks : 32 * ks + 8 * g));
     row_kend[i] = kend_of<PAGED>(a, q, tok);
   }
-  const int kmin = kend_of<PAGED>(a, q, 0);
+  const int kmin = kend_of<PAGED>(a, q, m0 / G);
   f32x4 acc[NQ][DT];
   float m_ref[NQ], l_part[NQ];
 #pragma unroll
@@ -203,9 +214,11 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  char* vs = smem + w * 32 * DH * 2;
-  const int j16 = n16;  // transposing read: row 4 g + j/4, 4 dims from 4 (j % 4) of each 16
-  const int vrow = 4 * g + (j16 >> 2);
+  char* vs = smem + w * 32 * spitch(DH);
+  // transposing read: lane j of a group points at row 4 g + j / 4, 4 dims from 4 (j % 4) of each 16
+  const char* vr = vs + (4 * g + (n16 >> 2)) * spitch(DH) + 8 * (n16 & 3);
+  const int ts = (int)a.tok_stride * (FP8 ? 1 : 2), cpr = DH * (FP8 ? 1 : 2) / 16;
+  const int koff = n16 * ts + (FP8 ? 32 : 16) * g, voff = lane / cpr * ts + 16 * (lane % cpr);
   const float c = a.c, thr = RESCALE_LOG2 / c;
 
   // tile i of this wavefront: keys start + 128 i + 32 w; lane l holds the page of group l % 2 of tile
@@ -219,7 +232,7 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
     if ((i & 31) == 0) pages(i);
     const int at = 2 * (i & 31);
     stream_load<DH, PAGED, FP8>(x, a, q, hk, first + 128 * i, end, __builtin_amdgcn_readlane(meta, at),
-                                __builtin_amdgcn_readlane(meta, at + 1), lane);
+                                __builtin_amdgcn_readlane(meta, at + 1), lane, koff, voff);
   };
   if (n_tiles > 0) load(0);
   for (int i = 0; i < n_tiles; ++i) {
@@ -293,10 +306,9 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
     // k slots of the value product: the four keys 4 g .. of group 0, then of group 1, on both sides
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      const int ch = 2 * d + ((j16 & 3) >> 1);
-      const char* at = vs + vrow * DH * 2 + 16 * sswz<DH>(vrow, ch) + 8 * (j16 & 1);
+      const char* at = vr + 32 * d;
       const s16x4 v2[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at),
-                           __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * DH * 2))};
+                           __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * spitch(DH)))};
       const bf16x8 vf = *reinterpret_cast<const bf16x8*>(v2);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) acc[n][d] = mfma16(vf, pb[n], acc[n][d]);
@@ -307,7 +319,7 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
   constexpr int PITCH = DH + 4;
   float* red = reinterpret_cast<float*>(smem);                // [4][16][PITCH]
   float* wml = red + 4 * 16 * PITCH;                          // [4][16][2]
-  static_assert((4 * 16 * PITCH + 128) * 4 <= 4 * BN * DH * 2, "fits the tiles' LDS");
+  static_assert(stream_lds(DH) <= 4 * BN * DH * 2, "fits the tile kernel's LDS");
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     float l = l_part[n];
@@ -329,7 +341,7 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
     __syncthreads();
     // thread: row tid / 16, DH / 16 dims
     constexpr int PER = DH / 16;
-    const int rr = tid >> 4, d0 = (tid & 15) * PER, row = 16 * n + rr;
+    const int rr = tid >> 4, d0 = (tid & 15) * PER, row = m0 + 16 * n + rr;
     top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 4; ++k) top = fmaxf(top, wml[(k * 16 + rr) * 2]);
@@ -569,67 +581,100 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
   }
 }
 
-// last request whose start (in units of 1 / scale rows, plus its number where by_tile) is not past x, or -1
-WAM_DEV int find_request(const RaggedArgs& a, int x, int G, bool by_tile, int lane) {
+// last request whose start is not past x, or -1; by row tiles (2^shift rows each) the first tile of request r is
+// floor(q_start[r] G / 2^shift) + r
+WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane) {
   int cnt = 0;
   for (int b = 0; b < a.R; b += 64) {
     const int r = b + lane;
     bool in = false;
-    if (r < a.R) in = by_tile ? (((int64_t)a.q_start[r] * G) >> 7) + r <= x : a.q_start[r] <= x;
+    if (r < a.R) in = shift ? (((int64_t)a.q_start[r] * G) >> shift) + r <= x : a.q_start[r] <= x;
     cnt += __popcll(__ballot(in));
   }
   return cnt - 1;
 }
-static_assert(RAGGED_ROWS == 128, "the shift above");
 
-template <int DH, bool PAGED, bool FP8>
-__global__ __launch_bounds__(NT, 2) void attn_ragged_kernel(const RaggedArgs a, const Parts pt) {
-  __shared__ __attribute__((aligned(16))) bf16 smem[4 * BN * DH];
-  const int G = a.Hq / a.Hkv, lane = threadIdx.x & 63;
-  int x, hk, split;
-  if (pt.by_xcd) {
+// A workgroup's work: its request, KV head, first row, and keys.
+struct Work {
+  Req q;
+  int r, hk, G, m0, split, start, end;
+  bool whole;  // the request has one part: the output itself is written
+};
+template <bool PAGED, int SHIFT>
+WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, Work& k) {
+  const int lane = threadIdx.x & 63;
+  k.G = a.Hq / a.Hkv;
+  int x;
+  if (SHIFT == 7) {
     // rows share keys with their neighbours: each XCD a contiguous range of (row tile, head) pairs
     const int nblk = gridDim.x, bi = blockIdx.x, xcd = bi & 7, per = nblk >> 3, rem = nblk & 7;
     const int lid = xcd * per + (xcd < rem ? xcd : rem) + (bi >> 3);
     x = lid % pt.tiles;
-    hk = lid / pt.tiles % a.Hkv;
-    split = lid / pt.tiles / a.Hkv;
+    k.hk = lid / pt.tiles % a.Hkv;
+    k.split = lid / pt.tiles / a.Hkv;
   } else {
-    hk = blockIdx.x % a.Hkv;
-    split = blockIdx.x / a.Hkv % pt.splits;
-    x = blockIdx.x / a.Hkv / pt.splits;
+    // the heads of the same keys, neighbours in memory, one after another on one XCD; parts and requests in turn over
+    // the XCDs
+    const int slot = blockIdx.x >> 3, part = slot / a.Hkv * 8 + (blockIdx.x & 7);
+    k.hk = slot % a.Hkv;
+    x = part / pt.splits;
+    k.split = (part + x) % pt.splits;  // (turned by the request, so that no XCD has all of the late, rarer parts)
   }
-  const int r = uniform(find_request(a, x, G, true, lane));
-  if (r < 0) return;
-  const Req q = request<PAGED>(a, r);
-  const int64_t m0 = ((int64_t)x - r - (((int64_t)q.q0 * G) >> 7)) * RAGGED_ROWS;
-  const int rows = q.n * G;
-  if (m0 < 0 || m0 >= rows) return;
-  const int start = split * pt.split_keys;
-  if (split > 0 && start >= q.keys) return;
-  const bool whole = q.keys <= pt.split_keys;
-  const int last = m0 + RAGGED_ROWS < rows ? (int)m0 + RAGGED_ROWS - 1 : rows - 1;
-  const int kmax = kend_of<PAGED>(a, q, last / G);
-  const int end = kmax - start < pt.split_keys ? kmax : start + pt.split_keys;
-  if (rows > RAGGED_STREAM)
-    tile_rows<DH, PAGED, FP8>(a, pt, q, r, hk, G, (int)m0, split, whole, start, end, smem);
-  else if (rows > 16)
-    stream_rows<DH, PAGED, FP8, 2>(a, pt, q, r, hk, G, split, whole, start, end, reinterpret_cast<char*>(smem));
-  else
-    stream_rows<DH, PAGED, FP8, 1>(a, pt, q, r, hk, G, split, whole, start, end, reinterpret_cast<char*>(smem));
+  if (x >= pt.tiles) return false;
+  k.r = uniform(find_request(a, x, k.G, SHIFT, lane));
+  if (k.r < 0) return false;
+  k.q = request<PAGED>(a, k.r);
+  const int64_t m0 = ((int64_t)x - k.r - (((int64_t)k.q.q0 * k.G) >> SHIFT)) * (1 << SHIFT);
+  const int rows = k.q.n * k.G;
+  if (m0 < 0 || m0 >= rows) return false;
+  k.m0 = (int)m0;
+  k.start = k.split * pt.split_keys;
+  if (k.split > 0 && k.start >= k.q.keys) return false;
+  k.whole = k.q.keys <= pt.split_keys;
+  const int last = rows - k.m0 > (1 << SHIFT) ? k.m0 + (1 << SHIFT) - 1 : rows - 1;
+  const int kmax = kend_of<PAGED>(a, k.q, last / k.G);
+  k.end = kmax - k.start < pt.split_keys ? kmax : k.start + pt.split_keys;
+  return true;
 }
 
-// o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over a row's parts, a wavefront per (token, head)
+// Requests with more than a few rows on average: 128 rows per workgroup; those with at most 32 are streamed.
 template <int DH, bool PAGED, bool FP8>
+__global__ __launch_bounds__(NT, 2) void ragged_tile_kernel(const RaggedArgs a, const Parts pt) {
+  __shared__ __attribute__((aligned(16))) bf16 smem[4 * BN * DH];
+  static_assert(RAGGED_ROWS == 128, "2^7 rows");
+  Work k;
+  if (!find_work<PAGED, 7>(a, pt, k)) return;
+  const int rows = k.q.n * k.G;
+  if (rows > RAGGED_STREAM)
+    tile_rows<DH, PAGED, FP8>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, smem);
+  else
+    stream_rows<DH, PAGED, FP8, 2>(a, pt, k.q, k.r, k.hk, k.G, 0, k.split, k.whole, k.start, k.end,
+                                   reinterpret_cast<char*>(smem));
+}
+
+// Few rows per request: 16 NQ per workgroup.
+template <int DH, bool PAGED, bool FP8, int NQ>
+__global__ __launch_bounds__(NT, NQ == 1 ? 3 : 2) void ragged_stream_kernel(const RaggedArgs a, const Parts pt) {
+  __shared__ __attribute__((aligned(16))) char smem[stream_lds(DH)];
+  Work k;
+  if (!find_work<PAGED, NQ == 1 ? 4 : 5>(a, pt, k)) return;
+  stream_rows<DH, PAGED, FP8, NQ>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, smem);
+}
+
+// o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over a row's parts: W wavefronts per (token, head), each
+// every W-th part, four loads in flight.
+template <int DH, bool PAGED, bool FP8, int W>
 __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, const Parts pt) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = (int)(id / a.Hq), h = (int)(id - (int64_t)t * a.Hq);
-  if (t >= a.T) return;
-  const int r = find_request(a, t, 1, false, lane);
-  if (r < 0) return;
-  const Req q = request<PAGED>(a, r);
-  if (t - q.q0 >= q.n || q.keys <= pt.split_keys) return;
+  __shared__ float red[4][DH];
+  constexpr int PER = DH / 64;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t id = (int64_t)blockIdx.x * (4 / W) + w / W;
+  const int t = (int)(id / a.Hq), h = (int)(id - (int64_t)t * a.Hq), sub = w % W;
+  const int r = t < a.T ? find_request(a, t, 1, 0, lane) : -1;
+  Req q{};
+  if (r >= 0) q = request<PAGED>(a, r);
+  const bool on = r >= 0 && t - q.q0 < q.n && q.keys > pt.split_keys;
+  if (!on) return;  // (W = 4: the same for the whole workgroup)
   const int n = (q.keys + pt.split_keys - 1) / pt.split_keys;
   float m = -INFINITY, l = 0.f;
   if (lane < n) {
@@ -641,13 +686,30 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
   for (int s = 1; s < 64; s <<= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
   const float f = l != 0.f ? exp2_fast((m - top) * a.c) : 0.f;
   const float sum = wave_sum(f * l);
-  constexpr int PER = DH / 64;
   float y[PER] = {};
-  for (int s = 0; s < n; ++s) {
-    const float fs = __shfl(f, s, 64);
-    if (fs == 0.f) continue;  // nothing was stored for a part without keys
+  const float* o = pt.o + id * pt.splits * DH + lane * PER;
+  for (int s0 = sub; s0 < n; s0 += 4 * W) {
+    float v[4][PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) y[e] += fs * pt.o[(id * pt.splits + s) * DH + lane * PER + e];
+    for (int j = 0; j < 4; ++j) {
+      const int s = s0 + j * W < n ? s0 + j * W : s0;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) v[j][e] = o[(int64_t)s * DH + e];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float fs = s0 + j * W < n ? __shfl(f, s0 + j * W, 64) : 0.f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) y[e] += fs != 0.f ? fs * v[j][e] : 0.f;  // (a part without keys stored nothing)
+    }
+  }
+  if (W > 1) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) red[w][lane * PER + e] = y[e];
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) y[e] = (red[0][lane * PER + e] + red[1][lane * PER + e]) + (red[2][lane * PER + e] + red[3][lane * PER + e]);
   }
   const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
   bf16* op = static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + lane * PER;
@@ -656,13 +718,18 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
 }
 
 template <int DH, bool PAGED, bool FP8>
-hipError_t launch(const RaggedArgs& a, const Parts& pt, hipStream_t s) {
-  const int64_t grid = (int64_t)pt.tiles * a.Hkv * pt.splits;
-  hipLaunchKernelGGL((attn_ragged_kernel<DH, PAGED, FP8>), dim3((unsigned)grid), dim3(NT), 0, s, a, pt);
+hipError_t launch(const RaggedArgs& a, const Parts& pt, int rows, hipStream_t s) {
+  const int64_t parts = (int64_t)pt.tiles * pt.splits;
+  const dim3 grid((unsigned)((rows == RAGGED_ROWS ? parts : (parts + 7) / 8 * 8) * a.Hkv)), block(NT);
+  if (rows == 16) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
+  else if (rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 2>), grid, block, 0, s, a, pt);
+  else hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8>), grid, block, 0, s, a, pt);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pt.splits == 1) return e;
-  hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8>), dim3((unsigned)(((int64_t)a.T * a.Hq + 3) / 4)), dim3(256), 0,
-                     s, a, pt);
+  const int64_t out = (int64_t)a.T * a.Hq;
+  // few parts or many rows: a wavefront for each row; else its parts over four
+  if (pt.splits <= 4) hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8, 1>), dim3((unsigned)((out + 3) / 4)), block, 0, s, a, pt);
+  else hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8, 4>), dim3((unsigned)out), block, 0, s, a, pt);
   return hipGetLastError();
 }
 
@@ -674,13 +741,12 @@ hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws
   pt.o = reinterpret_cast<float*>(static_cast<char*>(ws) + ragged_ml_bytes(p, a.T, a.Hq));
   pt.splits = p.splits;
   pt.split_keys = p.split_keys;
-  pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv);
-  pt.by_xcd = !p.few;
+  pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv, p.rows);
   if (a.table) {
-    if (a.k_exp) return launch<128, true, true>(a, pt, s);
-    return a.Dh == 128 ? launch<128, true, false>(a, pt, s) : launch<64, true, false>(a, pt, s);
+    if (a.k_exp) return launch<128, true, true>(a, pt, p.rows, s);
+    return a.Dh == 128 ? launch<128, true, false>(a, pt, p.rows, s) : launch<64, true, false>(a, pt, p.rows, s);
   }
-  return a.Dh == 128 ? launch<128, false, false>(a, pt, s) : launch<64, false, false>(a, pt, s);
+  return a.Dh == 128 ? launch<128, false, false>(a, pt, p.rows, s) : launch<64, false, false>(a, pt, p.rows, s);
 }
 
 }  // namespace wam

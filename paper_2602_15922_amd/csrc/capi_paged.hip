@@ -63,8 +63,8 @@ wam_status check_ragged(int32_t R, int32_t T, int32_t Hq, int32_t Hkv, int32_t D
   CHECK(Hq % Hkv == 0, WAM_EINVAL, "Hq=%d must be a multiple of Hkv=%d", Hq, Hkv);
   CHECK(R >= 0 && T >= 0 && max_k >= 0, WAM_EINVAL, "negative size (R=%d T=%d longest=%d)", R, T, max_k);
   CHECK(max_k <= 1 << 30, WAM_EUNSUPPORTED, "the longest key axis %d exceeds 2^30", max_k);
-  CHECK((int64_t)T * Hq <= INT32_MAX && ragged_tiles(R, T, Hq, Hkv) * Hkv <= INT32_MAX / RAGGED_MAX_SPLITS,
-        WAM_EUNSUPPORTED, "T * Hq and (R + T * Hq / Hkv / 128) * Hkv * 64 must stay below 2^31");
+  CHECK((int64_t)T * Hq <= INT32_MAX && ragged_tiles(R, T, Hq, Hkv, 16) * Hkv <= INT32_MAX / RAGGED_MAX_SPLITS,
+        WAM_EUNSUPPORTED, "T * Hq and (R + T * Hq / Hkv / 16) * Hkv * 64 must stay below 2^31");
   return WAM_OK;
 }
 wam_status check_rows(const void* q, const void* o, int64_t q_ts, int64_t o_ts, int64_t hd) {
