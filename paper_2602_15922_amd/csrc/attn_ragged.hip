@@ -76,10 +76,10 @@ WAM_DEV int kend_of(const RaggedArgs& a, const Req& q, int i) {
   return e < q.keys ? (int)e : q.keys;
 }
 
-// page of the 16 keys from `key` on (a multiple of 16), -1 where there is none
+// page of the 16 keys from `key` on (a multiple of 16), -1 where there is none (or the table ends)
 template <bool PAGED>
-WAM_DEV int page_of(const RaggedArgs& a, int r, int key, int end) {
-  if (key >= end) return -1;
+WAM_DEV int page_of(const RaggedArgs& a, int r, int key) {
+  if (key >= a.max_k) return -1;
   if (!PAGED) return 0;
   const int p = a.table[r * a.table_stride + fdiv(a.ps, key)];
   return (unsigned)p < (unsigned)a.n_pages ? p : -1;
@@ -185,12 +185,15 @@ WAM_DEV void stream_store_v(const StreamRegs<DH, FP8>& x, char* vs, int lane) {
     }
 }
 
+// key of the group whose page lane l holds, from the wavefront's first key on
+WAM_DEV int stream_key(int lane) { return 128 * (lane >> 1) + 16 * (lane & 1); }
+
 // LDS of the streaming path: four wavefronts' V tiles, or their 16 rows each of the join
 constexpr int stream_lds(int dh) { return (4 * 16 * (dh + 4) + 128) * 4 > 4 * 32 * spitch(dh) ? (4 * 16 * (dh + 4) + 128) * 4 : 4 * 32 * spitch(dh); }
 
 template <int DH, bool PAGED, bool FP8, int NQ>
 WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
-                         bool whole, int start, int end, char* smem) {
+                         bool whole, int start, int end, int meta, char* smem) {
   constexpr int KS = DH / 32, DT = DH / 16;
   const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, n16 = lane & 15;
   const int rows = q.n * G;
@@ -225,11 +228,10 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
   // base + l / 2, for 32 tiles at a time
   const int first = start + 32 * w;
   const int n_tiles = end > first ? (end - first + 127) / 128 : 0;
-  int meta = -1;
-  auto pages = [&](int base) { meta = page_of<PAGED>(a, r, first + 128 * (base + (lane >> 1)) + 16 * (lane & 1), end); };
+  auto pages = [&](int base) { meta = page_of<PAGED>(a, r, first + 128 * base + stream_key(lane)); };
   StreamRegs<DH, FP8> x;
   auto load = [&](int i) {
-    if ((i & 31) == 0) pages(i);
+    if (i > 0 && (i & 31) == 0) pages(i);
     const int at = 2 * (i & 31);
     stream_load<DH, PAGED, FP8>(x, a, q, hk, first + 128 * i, end, __builtin_amdgcn_readlane(meta, at),
                                 __builtin_amdgcn_readlane(meta, at + 1), lane, koff, voff);
@@ -481,11 +483,23 @@ WAM_DEV void ragged_tile(const char* Ks, const bf16x8* qf, f32x16* acc, float& m
   softmax_pv<DH>(s, Ks + BN * DH * 2, acc, m_ref, l_part, vofs, c, thr);
 }
 
-template <int DH, bool PAGED, bool FP8>
+// Wait for this wavefront's part of a tile (direct loads and LDS stores), then for the workgroup.
+WAM_DEV void tile_arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// GROUPS = 2: the key tiles go in turn to two groups of four wavefronts, each with its own pair of LDS buffers, and the
+// groups' states are joined in LDS at the end: two wavefronts per SIMD where there are too few workgroups for two on a
+// CU, without parts in memory.
+template <int DH, bool PAGED, bool FP8, int GROUPS>
 WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
-                       bool whole, int start, int end, bf16* smem) {
+                       bool whole, int start, int end, int meta, bf16* smem_all) {
   constexpr int KS = DH / 16, MT = DH / 32, TILE = 2 * BN * DH;
-  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), hh = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
+  const int w = uniform(tid >> 6) & 3, grp = GROUPS == 1 ? 0 : uniform(tid >> 8);
+  bf16* smem = smem_all + grp * 2 * TILE;
   const int rows = q.n * G;
   const int qrow = m0 + 32 * w + l32, qc = qrow < rows ? qrow : rows - 1, tok = qc / G, head = hk * G + qc - tok * G;
   const int row_kend = kend_of<PAGED>(a, q, tok);
@@ -501,10 +515,10 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) kofs[ks] = l32 * DH * 2 + kswz<DH>(l32, 2 * ks + hh) * 16;
   {
-    const int grp = lane >> 4, j16 = lane & 15, r0 = 4 * (grp >> 1) + (j16 >> 2);
+    const int l16 = lane >> 4, j16 = lane & 15, r0 = 4 * (l16 >> 1) + (j16 >> 2);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int col = 32 * mt + 16 * (grp & 1) + 4 * (j16 & 3);
+      const int col = 32 * mt + 16 * (l16 & 1) + 4 * (j16 & 3);
       vofs[mt] = r0 * DH * 2 + vswz<DH>(r0, col >> 3) * 16 + 8 * ((col >> 2) & 1);
     }
   }
@@ -518,72 +532,132 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
   const int n_plain = kmin / BN;  // tiles before it hide no key from any row
   Fetch<DH, PAGED, FP8> f;
   f.init(a, lane);
-  // pages of a window of 16 tiles, lane l: keys 16 l .. of it; and of the next window
-  int meta = page_of<PAGED>(a, r, start + 16 * lane, end), meta_next = -1;
-  auto fetch = [&](int t, int wend) {
+  // meta: the pages of a window of 16 tiles, lane l keys 16 l .. of it; and of the next window
+  int meta_next = -1;
+  auto fetch = [&](int t, int cur, int wend) {
     const int key = t * BN + 16 * w, pg = __builtin_amdgcn_readlane(t < wend ? meta : meta_next, (4 * (t - t0) + w) & 63);
     const int nv = pg < 0 ? 0 : clampi(end - key, 0, 16);
-    f.load(a, q, smem + ((t - t0) & 1) * TILE, key, pg, nv, hk, w, lane);
+    f.load(a, q, smem + cur * TILE, key, pg, nv, hk, w, lane);
   };
-  if (nt > t0) {
-    fetch(t0, t0 + 16);
+  // this group's tiles: t0 + grp, then every GROUPS-th; two at a time, one per buffer
+  if (t0 + grp < nt) {
+    fetch(t0 + grp, 0, t0 + 16);
     f.store(smem, w, lane);
   }
-  tile_sync();
+  tile_arrived();
   for (int wb = t0; wb < nt; wb += 16) {
     const int we = wb + 16 < nt ? wb + 16 : nt;
-    meta_next = page_of<PAGED>(a, r, (wb + 16) * BN + 16 * lane, end);
+    meta_next = page_of<PAGED>(a, r, (wb + 16) * BN + 16 * lane);
     // (groups past the end count as present: the rows' prefixes hide them)
     const uint64_t there = __ballot(meta >= 0 || wb * BN + 16 * lane >= end);
     const int plain = ~there == 0 ? (n_plain < we ? n_plain : we) : wb;
-    int t = wb;
+    int tb = wb;  // the groups' tiles tb .. tb + GROUPS - 1
     auto step = [&](int cur, auto mask) {
-      if (t + 1 < nt) fetch(t + 1, wb + 16);
-      const char* Ks = reinterpret_cast<const char*>(smem + cur * TILE);
-      ragged_tile<DH, decltype(mask)::value>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend,
-                                             (int)(there >> (4 * (t - wb))) & 15, hh);
-      if (t + 1 < nt) f.store(smem + (cur ^ 1) * TILE, w, lane);
-      tile_sync();
-      ++t;
+      const int t = tb + grp;
+      if (GROUPS == 1 || t < nt) {
+        if (t + GROUPS < nt) fetch(t + GROUPS, cur ^ 1, wb + 16);
+        const char* Ks = reinterpret_cast<const char*>(smem + cur * TILE);
+        ragged_tile<DH, decltype(mask)::value>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend,
+                                               (int)(there >> (4 * (t - wb))) & 15, hh);
+        if (t + GROUPS < nt) f.store(smem + (cur ^ 1) * TILE, w, lane);
+      }
+      tile_arrived();
+      tb += GROUPS;
     };
-    while (t + 2 <= plain) {
+    while (tb + 2 * GROUPS <= plain) {
       step(0, std::false_type{});
       step(1, std::false_type{});
     }
-    while (t < we) step((t - t0) & 1, std::true_type{});
+    while (tb < we) step((tb - t0) / GROUPS & 1, std::true_type{});
     meta = meta_next;
   }
 
-  const float l = l_part + other_half(l_part);
-  if (qrow >= rows) return;
-  if (whole) {
-    const float inv = l > 0.f ? (FP8 ? a.v_scale : 1.f) / l : 0.f;
-    bf16* ob = static_cast<bf16*>(a.o) + (q.q0 + tok) * a.o_ts + head * DH;
+  float l = l_part + other_half(l_part);
+  if constexpr (GROUPS == 2) {
+    // the second group's state through the first's buffers, register by register (the same lanes hold the same rows)
+    float* mine = reinterpret_cast<float*>(smem_all) + w * (16 * MT * 64) + lane;
+    float* stat = reinterpret_cast<float*>(smem_all + 2 * TILE) + w * 128 + lane;
+    if (grp == 1) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[(16 * mt + e) * 64] = acc[mt][e];
+      stat[0] = m_ref;
+      stat[64] = l;
+    }
+    __syncthreads();
+    if (grp == 1) return;
+    const float m2 = stat[0], l2 = stat[64], top = fmaxf(m_ref, m2);
+    const float f1 = m_ref == -INFINITY ? 0.f : exp2_fast((m_ref - top) * c);
+    const float f2 = m2 == -INFINITY ? 0.f : exp2_fast((m2 - top) * c);
+    m_ref = top;
+    l = l * f1 + l2 * f2;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int rr = 0; rr < 4; ++rr)
-        *reinterpret_cast<bf16x4*>(ob + 32 * mt + 8 * rr + 4 * hh) =
+      for (int e = 0; e < 16; ++e) acc[mt][e] = acc[mt][e] * f1 + mine[(16 * mt + e) * 64] * f2;
+    asm volatile("" ::: "memory");  // (each wavefront reads and then overwrites its own quarter)
+  }
+  // The output through LDS (the key tiles are done with), so that a row leaves in whole lines: a lane holds 4 dims here and
+  // there of one row; the wavefront's 32 rows go to its quarter of LDS, 16-byte chunks XOR-swizzled by the row (written
+  // 8 bytes per lane, 32 rows; read back one row per 16 lanes).  whole: bf16; else fp32, in two halves of the dims.
+  char* my = reinterpret_cast<char*>(smem) + w * (BN * DH * 2);
+  constexpr int CH = DH / 8, RPI = 64 / CH;  // 16-byte chunks of a row of DH bf16 (or DH / 2 fp32), rows per instruction
+  const auto put = [&](auto&& chunk_out) {  // chunk_out(row's index, token, head, chunk, 16 bytes)
+    asm volatile("" ::: "memory");  // other lanes' rows: no LDS access moves across (they run in order)
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int rr = RPI * i + lane / CH, ch = lane % CH, row = m0 + 32 * w + rr;
+      const u32x4v v = *reinterpret_cast<const u32x4v*>(my + rr * DH * 2 + 16 * (ch ^ (rr & (CH - 1))));
+      if (row < rows) {
+        const int tk = row / G;
+        chunk_out((int64_t)q.q0 + tk, hk * G + row - tk * G, ch, v);
+      }
+    }
+    asm volatile("" ::: "memory");
+  };
+  if (whole) {
+    const float inv = l > 0.f ? (FP8 ? a.v_scale : 1.f) / l : 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const int ch = 4 * mt + rr;  // dims 8 ch + 4 hh ..
+        *reinterpret_cast<bf16x4*>(my + l32 * DH * 2 + 16 * (ch ^ (l32 & (CH - 1))) + 8 * hh) =
             bf16x4{(bf16)(acc[mt][4 * rr + 0] * inv), (bf16)(acc[mt][4 * rr + 1] * inv),
                    (bf16)(acc[mt][4 * rr + 2] * inv), (bf16)(acc[mt][4 * rr + 3] * inv)};
+      }
+    put([&](int64_t tk, int h, int ch, u32x4v v) {
+      *reinterpret_cast<u32x4v*>(static_cast<bf16*>(a.o) + tk * a.o_ts + h * DH + 8 * ch) = v;
+    });
   } else {
-    const int64_t id = ((int64_t)(q.q0 + tok) * a.Hq + head) * pt.splits + split;
-    if (hh == 0) {
+    if (hh == 0 && qrow < rows) {
+      const int64_t id = ((int64_t)(q.q0 + tok) * a.Hq + head) * pt.splits + split;
       pt.ml[2 * id] = m_ref;
       pt.ml[2 * id + 1] = l;
     }
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int rr = 0; rr < 4; ++rr)
-        *reinterpret_cast<f32x4*>(pt.o + id * DH + 32 * mt + 8 * rr + 4 * hh) =
-            f32x4{acc[mt][4 * rr + 0], acc[mt][4 * rr + 1], acc[mt][4 * rr + 2], acc[mt][4 * rr + 3]};
+      for (int mt = half * MT / 2; mt < (half + 1) * MT / 2; ++mt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const int ch = 8 * (mt - half * MT / 2) + 2 * rr + hh;  // dims DH / 2 half + 4 ch ..
+          *reinterpret_cast<f32x4*>(my + l32 * DH * 2 + 16 * (ch ^ (l32 & (CH - 1)))) =
+              f32x4{acc[mt][4 * rr + 0], acc[mt][4 * rr + 1], acc[mt][4 * rr + 2], acc[mt][4 * rr + 3]};
+        }
+      put([&](int64_t tk, int h, int ch, u32x4v v) {
+        const int64_t id = (tk * a.Hq + h) * pt.splits + split;
+        *reinterpret_cast<u32x4v*>(pt.o + id * DH + half * (DH / 2) + 4 * ch) = v;
+      });
+    }
   }
 }
 
 // last request whose start is not past x, or -1; by row tiles (2^shift rows each) the first tile of request r is
 // floor(q_start[r] G / 2^shift) + r
 WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane) {
+  if (a.R == 1) return 0;  // (rows before it or past it are none of its)
   int cnt = 0;
   for (int b = 0; b < a.R; b += 64) {
     const int r = b + lane;
@@ -598,6 +672,7 @@ WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane)
 struct Work {
   Req q;
   int r, hk, G, m0, split, start, end;
+  int meta;    // lane: page of a group of the first keys
   bool whole;  // the request has one part: the output itself is written
 };
 template <bool PAGED, int SHIFT>
@@ -623,12 +698,15 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, Work& k) {
   if (x >= pt.tiles) return false;
   k.r = uniform(find_request(a, x, k.G, SHIFT, lane));
   if (k.r < 0) return false;
+  k.start = k.split * pt.split_keys;
+  // the first keys' pages, before the request's own lengths are there (the table's row is)
+  const int w = uniform(threadIdx.x >> 6);
+  k.meta = page_of<PAGED>(a, k.r, k.start + (SHIFT == 7 ? 16 * lane : 32 * w + stream_key(lane)));
   k.q = request<PAGED>(a, k.r);
   const int64_t m0 = ((int64_t)x - k.r - (((int64_t)k.q.q0 * k.G) >> SHIFT)) * (1 << SHIFT);
   const int rows = k.q.n * k.G;
   if (m0 < 0 || m0 >= rows) return false;
   k.m0 = (int)m0;
-  k.start = k.split * pt.split_keys;
   if (k.split > 0 && k.start >= k.q.keys) return false;
   k.whole = k.q.keys <= pt.split_keys;
   const int last = rows - k.m0 > (1 << SHIFT) ? k.m0 + (1 << SHIFT) - 1 : rows - 1;
@@ -638,17 +716,18 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, Work& k) {
 }
 
 // Requests with more than a few rows on average: 128 rows per workgroup; those with at most 32 are streamed.
-template <int DH, bool PAGED, bool FP8>
-__global__ __launch_bounds__(NT, 2) void ragged_tile_kernel(const RaggedArgs a, const Parts pt) {
-  __shared__ __attribute__((aligned(16))) bf16 smem[4 * BN * DH];
+template <int DH, bool PAGED, bool FP8, int GROUPS>
+__global__ __launch_bounds__(NT * GROUPS, 2) void ragged_tile_kernel(const RaggedArgs a, const Parts pt) {
+  __shared__ __attribute__((aligned(16))) bf16 smem[GROUPS * 4 * BN * DH];
   static_assert(RAGGED_ROWS == 128, "2^7 rows");
   Work k;
   if (!find_work<PAGED, 7>(a, pt, k)) return;
   const int rows = k.q.n * k.G;
-  if (rows > RAGGED_STREAM)
-    tile_rows<DH, PAGED, FP8>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, smem);
-  else
+  if (GROUPS == 2 || rows > RAGGED_STREAM)
+    tile_rows<DH, PAGED, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem);
+  else if constexpr (GROUPS == 1)
     stream_rows<DH, PAGED, FP8, 2>(a, pt, k.q, k.r, k.hk, k.G, 0, k.split, k.whole, k.start, k.end,
+                                   page_of<PAGED>(a, k.r, k.start + 32 * uniform(threadIdx.x >> 6) + stream_key(threadIdx.x & 63)),
                                    reinterpret_cast<char*>(smem));
 }
 
@@ -658,24 +737,30 @@ __global__ __launch_bounds__(NT, NQ == 1 ? 3 : 2) void ragged_stream_kernel(cons
   __shared__ __attribute__((aligned(16))) char smem[stream_lds(DH)];
   Work k;
   if (!find_work<PAGED, NQ == 1 ? 4 : 5>(a, pt, k)) return;
-  stream_rows<DH, PAGED, FP8, NQ>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, smem);
+  stream_rows<DH, PAGED, FP8, NQ>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem);
 }
 
-// o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over a row's parts: W wavefronts per (token, head), each
-// every W-th part, four loads in flight.
-template <int DH, bool PAGED, bool FP8, int W>
-__global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, const Parts pt) {
+// The join: o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over the parts s of a row, in their order.
+// Two forms: for few rows a workgroup for each, its parts over four wavefronts (the chain of loads is what takes the
+// time); for many a thread for four dims of a row, a workgroup for some heads of a token.
+template <bool PAGED>
+WAM_DEV int parts_of(const RaggedArgs& a, const Parts& pt, int t, int lane) {  // 0: nothing to join
+  const int r = uniform(find_request(a, t, 1, 0, lane));
+  if (r < 0) return 0;
+  const Req q = request<PAGED>(a, r);
+  if (t < q.q0 || t - q.q0 >= q.n || q.keys <= pt.split_keys) return 0;
+  return (q.keys + pt.split_keys - 1) / pt.split_keys;
+}
+
+template <int DH, bool PAGED, bool FP8>
+__global__ __launch_bounds__(256) void ragged_join_few_kernel(const RaggedArgs a, const Parts pt) {
   __shared__ float red[4][DH];
   constexpr int PER = DH / 64;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t id = (int64_t)blockIdx.x * (4 / W) + w / W;
-  const int t = (int)(id / a.Hq), h = (int)(id - (int64_t)t * a.Hq), sub = w % W;
-  const int r = t < a.T ? find_request(a, t, 1, 0, lane) : -1;
-  Req q{};
-  if (r >= 0) q = request<PAGED>(a, r);
-  const bool on = r >= 0 && t - q.q0 < q.n && q.keys > pt.split_keys;
-  if (!on) return;  // (W = 4: the same for the whole workgroup)
-  const int n = (q.keys + pt.split_keys - 1) / pt.split_keys;
+  const int64_t id = blockIdx.x;
+  const int t = (int)(id / a.Hq), h = (int)(id - (int64_t)t * a.Hq);
+  const int n = parts_of<PAGED>(a, pt, t, lane);
+  if (n == 0) return;
   float m = -INFINITY, l = 0.f;
   if (lane < n) {
     m = pt.ml[2 * (id * pt.splits + lane)];
@@ -688,48 +773,75 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
   const float sum = wave_sum(f * l);
   float y[PER] = {};
   const float* o = pt.o + id * pt.splits * DH + lane * PER;
-  for (int s0 = sub; s0 < n; s0 += 4 * W) {
+  for (int s0 = w; s0 < n; s0 += 16) {
     float v[4][PER];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int s = s0 + j * W < n ? s0 + j * W : s0;
+      const int s = s0 + 4 * j < n ? s0 + 4 * j : s0;
 #pragma unroll
       for (int e = 0; e < PER; ++e) v[j][e] = o[(int64_t)s * DH + e];
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float fs = s0 + j * W < n ? __shfl(f, s0 + j * W, 64) : 0.f;
+      const float fs = s0 + 4 * j < n ? __shfl(f, s0 + 4 * j, 64) : 0.f;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) y[e] += fs != 0.f ? fs * v[j][e] : 0.f;  // (a part without keys stored nothing)
+      for (int e = 0; e < PER; ++e) y[e] += fs != 0.f ? fs * v[j][e] : 0.f;
     }
   }
-  if (W > 1) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) red[w][lane * PER + e] = y[e];
-    __syncthreads();
-    if (w > 0) return;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) y[e] = (red[0][lane * PER + e] + red[1][lane * PER + e]) + (red[2][lane * PER + e] + red[3][lane * PER + e]);
-  }
+  for (int e = 0; e < PER; ++e) red[w][lane * PER + e] = y[e];
+  __syncthreads();
+  if (w > 0) return;
   const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
   bf16* op = static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + lane * PER;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) op[e] = (bf16)(y[e] * inv);
+  for (int e = 0; e < PER; ++e) {
+    const int i = lane * PER + e;
+    op[e] = (bf16)(((red[0][i] + red[1][i]) + (red[2][i] + red[3][i])) * inv);
+  }
 }
 
 template <int DH, bool PAGED, bool FP8>
-hipError_t launch(const RaggedArgs& a, const Parts& pt, int rows, hipStream_t s) {
+__global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, const Parts pt) {
+  constexpr int LPH = DH / 4, HEADS = 256 / LPH;  // threads of a head, heads of a workgroup
+  const int t = blockIdx.x, n = parts_of<PAGED>(a, pt, t, threadIdx.x & 63), d = threadIdx.x % LPH * 4;
+  if (n == 0) return;
+  const int h = blockIdx.y * HEADS + threadIdx.x / LPH;
+  if (h < a.Hq) {
+    const int64_t id = ((int64_t)t * a.Hq + h) * pt.splits;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) top = fmaxf(top, pt.ml[2 * (id + s)]);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+      const float m = pt.ml[2 * (id + s)], l = pt.ml[2 * (id + s) + 1], f = l != 0.f ? exp2_fast((m - top) * a.c) : 0.f;
+      const f32x4 v = *reinterpret_cast<const f32x4*>(pt.o + (id + s) * DH + d);
+      sum += f * l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += f != 0.f ? f * v[e] : 0.f;
+    }
+    const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
+    *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + d) =
+        bf16x4{(bf16)(y[0] * inv), (bf16)(y[1] * inv), (bf16)(y[2] * inv), (bf16)(y[3] * inv)};
+  }
+}
+
+template <int DH, bool PAGED, bool FP8>
+hipError_t launch(const RaggedArgs& a, const Parts& pt, int rows, int groups, hipStream_t s) {
   const int64_t parts = (int64_t)pt.tiles * pt.splits;
   const dim3 grid((unsigned)((rows == RAGGED_ROWS ? parts : (parts + 7) / 8 * 8) * a.Hkv)), block(NT);
   if (rows == 16) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
   else if (rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 2>), grid, block, 0, s, a, pt);
-  else hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8>), grid, block, 0, s, a, pt);
+  else if (groups == 1) hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
+  else hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8, 2>), grid, dim3(2 * NT), 0, s, a, pt);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pt.splits == 1) return e;
   const int64_t out = (int64_t)a.T * a.Hq;
-  // few parts or many rows: a wavefront for each row; else its parts over four
-  if (pt.splits <= 4) hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8, 1>), dim3((unsigned)((out + 3) / 4)), block, 0, s, a, pt);
-  else hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8, 4>), dim3((unsigned)out), block, 0, s, a, pt);
+  constexpr int HEADS = 256 / (DH / 4);
+  if (out <= 4096) hipLaunchKernelGGL((ragged_join_few_kernel<DH, PAGED, FP8>), dim3((unsigned)out), block, 0, s, a, pt);
+  else hipLaunchKernelGGL((ragged_join_kernel<DH, PAGED, FP8>), dim3((unsigned)a.T, (unsigned)((a.Hq + HEADS - 1) / HEADS)), block, 0, s, a,
+                          pt);
   return hipGetLastError();
 }
 
@@ -743,10 +855,10 @@ hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws
   pt.split_keys = p.split_keys;
   pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv, p.rows);
   if (a.table) {
-    if (a.k_exp) return launch<128, true, true>(a, pt, p.rows, s);
-    return a.Dh == 128 ? launch<128, true, false>(a, pt, p.rows, s) : launch<64, true, false>(a, pt, p.rows, s);
+    if (a.k_exp) return launch<128, true, true>(a, pt, p.rows, p.groups, s);
+    return a.Dh == 128 ? launch<128, true, false>(a, pt, p.rows, p.groups, s) : launch<64, true, false>(a, pt, p.rows, p.groups, s);
   }
-  return a.Dh == 128 ? launch<128, false, false>(a, pt, p.rows, s) : launch<64, false, false>(a, pt, p.rows, s);
+  return a.Dh == 128 ? launch<128, false, false>(a, pt, p.rows, p.groups, s) : launch<64, false, false>(a, pt, p.rows, p.groups, s);
 }
 
 }  // namespace wam

@@ -175,7 +175,7 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
 
 size_t wam_attn_paged_workspace_bytes(const wam_attn_paged_desc* desc, const wam_paged_cache* cache) {
   if (!desc || !cache || check_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv) != WAM_OK) return 0;
-  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, desc->max_kv), desc->T, desc->Hq, cache->Dh);
+  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv), desc->T, desc->Hq, cache->Dh);
 }
 
 wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache* cache, const void* q,
@@ -195,7 +195,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   TRY(opt_ints(q_len, "q_len"));
   TRY(need_ints(kv_len, "kv_len"));
   if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
-  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, d.max_kv);
+  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
   TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
   RaggedArgs a{};
   a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
@@ -216,7 +216,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
 
 size_t wam_attn_cross_workspace_bytes(const wam_attn_cross_desc* desc) {
   if (!desc || check_ragged(desc->R, desc->T, desc->Hq, desc->Hkv, desc->Dh, desc->max_k) != WAM_OK) return 0;
-  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, desc->Hkv, desc->max_k), desc->T, desc->Hq, desc->Dh);
+  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, desc->Hkv, desc->Dh, desc->max_k), desc->T, desc->Hq, desc->Dh);
 }
 
 wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const void* k, const void* v,
@@ -239,7 +239,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   TRY(opt_ints(q_len, "q_len"));
   TRY(need_ints(k_start, "k_start"));
   TRY(opt_ints(k_len, "k_len"));
-  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, d.Hkv, d.max_k);
+  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, d.Hkv, d.Dh, d.max_k);
   TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, d.Dh)));
   RaggedArgs a{};
   a.q = q; a.k = k; a.v = v; a.o = o;
