@@ -32,11 +32,13 @@ struct Parts {
   float* ml;  // [row][splits][2]: reference and sum
   float* o;   // [row][splits][Dh]
   int splits, split_keys, tiles;
+  FastDiv by_splits, by_tiles, by_heads;
 };
 
 WAM_DEV int fdiv(const FastDiv& f, int n) {
   return f.d == 1 ? n : (int)(__umulhi((uint32_t)n, f.mul) >> f.shift);
 }
+WAM_DEV int fdiv_rest(const FastDiv& f, int n) { return n - fdiv(f, n) * (int)f.d; }
 WAM_DEV int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 WAM_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -48,31 +50,34 @@ struct Req {
 };
 template <bool PAGED>
 WAM_DEV Req request(const RaggedArgs& a, int r) {
+  // every load before any use: one trip to memory
+  const int32_t* qn = a.q_len ? a.q_len : a.q_start;
+  const int32_t* kn = PAGED || a.k_len ? a.k_len + r : a.k_start + r + 1;
+  const int32_t* kf = PAGED ? a.k_len : a.k_start;
+  const int q0 = a.q_start[r], q1 = a.q_start[r + 1], n = qn[r], klen = *kn, kfirst = kf[r];
   Req q;
-  q.q0 = a.q_start[r];
-  const int end = clampi(a.q_start[r + 1], 0, a.T);
-  q.n = q.q0 < 0 || q.q0 >= end ? 0 : end - q.q0;
-  if (a.q_len) q.n = clampi(a.q_len[r], 0, q.n);
+  const int end = clampi(q1, 0, a.T), room = q0 < 0 || q0 >= end ? 0 : end - q0;
+  q.q0 = q0;
+  q.n = a.q_len ? clampi(n, 0, room) : room;
   if (PAGED) {
     q.k0 = 0;
-    q.kv = a.k_len[r];
-    q.keys = clampi(q.kv, 0, a.max_k);
+    q.kv = klen;
+    q.keys = clampi(klen, 0, a.max_k);
   } else {
-    const int k0 = clampi(a.k_start[r], 0, a.S);
-    const int64_t len = a.k_len ? a.k_len[r] : (int64_t)a.k_start[r + 1] - k0;
-    const int room = a.S - k0 < a.max_k ? a.S - k0 : a.max_k;
+    const int k0 = clampi(kfirst, 0, a.S), most = a.S - k0 < a.max_k ? a.S - k0 : a.max_k;
+    const int64_t len = a.k_len ? klen : (int64_t)klen - k0;
     q.k0 = k0;
-    q.kv = q.keys = len < 0 ? 0 : (len < room ? (int)len : room);
+    q.kv = q.keys = len < 0 ? 0 : (len < most ? (int)len : most);
   }
   return q;
 }
 // keys that token i of the request sees (a prefix)
 template <bool PAGED>
 WAM_DEV int kend_of(const RaggedArgs& a, const Req& q, int i) {
-  if (!PAGED || a.chunk == 0) return q.keys;
+  if (!PAGED || a.chunk.d == 0) return q.keys;
   const int64_t p = (int64_t)q.kv - q.n + i;
   if (p < 0) return 0;
-  const int64_t e = (int64_t)((uint32_t)p / (uint32_t)a.chunk + 1) * a.chunk;
+  const int64_t e = ((int64_t)fdiv(a.chunk, (int)p) + 1) * a.chunk.d;
   return e < q.keys ? (int)e : q.keys;
 }
 
@@ -201,13 +206,13 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
   int row_kend[NQ];
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
-    const int row = m0 + 16 * i + n16 < rows ? m0 + 16 * i + n16 : rows - 1, tok = row / G;
+    const int row = m0 + 16 * i + n16 < rows ? m0 + 16 * i + n16 : rows - 1, tok = fdiv(a.group, row);
     const bf16* qp = static_cast<const bf16*>(a.q) + (q.q0 + tok) * a.q_ts + (hk * G + row - tok * G) * DH;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[i][ks] = load_bf16x8(qp + (FP8 ? 32 * g + 8 * ks : 32 * ks + 8 * g));
     row_kend[i] = kend_of<PAGED>(a, q, tok);
   }
-  const int kmin = kend_of<PAGED>(a, q, m0 / G);
+  const int kmin = kend_of<PAGED>(a, q, fdiv(a.group, m0));
   f32x4 acc[NQ][DT];
   float m_ref[NQ], l_part[NQ];
 #pragma unroll
@@ -360,7 +365,7 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
 #pragma unroll
       for (int e = 0; e < PER; ++e) y[e] += red[(k * 16 + rr) * PITCH + d0 + e];
     if (row < rows) {
-      const int tok = row / G, h = hk * G + row - tok * G;
+      const int tok = fdiv(a.group, row), h = hk * G + row - tok * G;
       if (whole) {
         const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
         bf16* op = static_cast<bf16*>(a.o) + (q.q0 + tok) * a.o_ts + h * DH + d0;
@@ -501,9 +506,9 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
   const int w = uniform(tid >> 6) & 3, grp = GROUPS == 1 ? 0 : uniform(tid >> 8);
   bf16* smem = smem_all + grp * 2 * TILE;
   const int rows = q.n * G;
-  const int qrow = m0 + 32 * w + l32, qc = qrow < rows ? qrow : rows - 1, tok = qc / G, head = hk * G + qc - tok * G;
+  const int qrow = m0 + 32 * w + l32, qc = qrow < rows ? qrow : rows - 1, tok = fdiv(a.group, qc), head = hk * G + qc - tok * G;
   const int row_kend = kend_of<PAGED>(a, q, tok);
-  const int kmin = kend_of<PAGED>(a, q, m0 / G);
+  const int kmin = kend_of<PAGED>(a, q, fdiv(a.group, m0));
   bf16x8 qf[KS];
   {
     const bf16* qp = static_cast<const bf16*>(a.q) + (q.q0 + tok) * a.q_ts + head * DH + 8 * hh;
@@ -610,7 +615,7 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
       const int rr = RPI * i + lane / CH, ch = lane % CH, row = m0 + 32 * w + rr;
       const u32x4v v = *reinterpret_cast<const u32x4v*>(my + rr * DH * 2 + 16 * (ch ^ (rr & (CH - 1))));
       if (row < rows) {
-        const int tk = row / G;
+        const int tk = fdiv(a.group, row);
         chunk_out((int64_t)q.q0 + tk, hk * G + row - tk * G, ch, v);
       }
     }
@@ -678,22 +683,24 @@ struct Work {
 template <bool PAGED, int SHIFT>
 WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, Work& k) {
   const int lane = threadIdx.x & 63;
-  k.G = a.Hq / a.Hkv;
+  k.G = (int)a.group.d;
   int x;
   if (SHIFT == 7) {
     // rows share keys with their neighbours: each XCD a contiguous range of (row tile, head) pairs
     const int nblk = gridDim.x, bi = blockIdx.x, xcd = bi & 7, per = nblk >> 3, rem = nblk & 7;
     const int lid = xcd * per + (xcd < rem ? xcd : rem) + (bi >> 3);
-    x = lid % pt.tiles;
-    k.hk = lid / pt.tiles % a.Hkv;
-    k.split = lid / pt.tiles / a.Hkv;
+    const int column = fdiv(pt.by_tiles, lid);
+    x = lid - column * pt.tiles;
+    k.split = fdiv(pt.by_heads, column);
+    k.hk = column - k.split * a.Hkv;
   } else {
     // the heads of the same keys, neighbours in memory, one after another on one XCD; parts and requests in turn over
     // the XCDs
-    const int slot = blockIdx.x >> 3, part = slot / a.Hkv * 8 + (blockIdx.x & 7);
-    k.hk = slot % a.Hkv;
-    x = part / pt.splits;
-    k.split = (part + x) % pt.splits;  // (turned by the request, so that no XCD has all of the late, rarer parts)
+    const int slot = blockIdx.x >> 3, column = fdiv(pt.by_heads, slot), part = column * 8 + (blockIdx.x & 7);
+    k.hk = slot - column * a.Hkv;
+    x = fdiv(pt.by_splits, part);
+    const int turned = part - x * pt.splits + fdiv_rest(pt.by_splits, x);
+    k.split = turned < pt.splits ? turned : turned - pt.splits;  // (by the request: no XCD has all of the late, rarer parts)
   }
   if (x >= pt.tiles) return false;
   k.r = uniform(find_request(a, x, k.G, SHIFT, lane));
@@ -710,7 +717,7 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, Work& k) {
   if (k.split > 0 && k.start >= k.q.keys) return false;
   k.whole = k.q.keys <= pt.split_keys;
   const int last = rows - k.m0 > (1 << SHIFT) ? k.m0 + (1 << SHIFT) - 1 : rows - 1;
-  const int kmax = kend_of<PAGED>(a, k.q, last / k.G);
+  const int kmax = kend_of<PAGED>(a, k.q, fdiv(a.group, last));
   k.end = kmax - k.start < pt.split_keys ? kmax : k.start + pt.split_keys;
   return true;
 }
@@ -854,6 +861,9 @@ hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws
   pt.splits = p.splits;
   pt.split_keys = p.split_keys;
   pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv, p.rows);
+  pt.by_splits = fast_div(p.splits);
+  pt.by_tiles = fast_div(pt.tiles);
+  pt.by_heads = fast_div(a.Hkv);
   if (a.table) {
     if (a.k_exp) return launch<128, true, true>(a, pt, p.rows, p.groups, s);
     return a.Dh == 128 ? launch<128, true, false>(a, pt, p.rows, p.groups, s) : launch<64, true, false>(a, pt, p.rows, p.groups, s);

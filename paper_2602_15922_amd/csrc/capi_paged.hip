@@ -204,7 +204,9 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   a.q_start = q_start; a.q_len = q_len; a.k_len = kv_len;
   a.table_stride = d.table_stride; a.q_ts = d.q_tok_stride; a.o_ts = d.o_tok_stride;
   a.page_stride = c.page_stride; a.tok_stride = c.tok_stride; a.head_stride = c.head_stride;
-  a.R = d.R; a.T = d.T; a.Hq = d.Hq; a.Hkv = c.Hkv; a.Dh = c.Dh; a.chunk = d.chunk; a.n_pages = c.n_pages;
+  a.R = d.R; a.T = d.T; a.Hq = d.Hq; a.Hkv = c.Hkv; a.Dh = c.Dh; a.n_pages = c.n_pages;
+  a.group = fast_div((uint32_t)(d.Hq / c.Hkv));
+  if (d.chunk > 0) a.chunk = fast_div((uint32_t)d.chunk);
   const int64_t width = (int64_t)d.max_pages * c.page_size;
   a.max_k = (int32_t)(width < d.max_kv ? width : d.max_kv);
   a.ps = fast_div((uint32_t)c.page_size);
@@ -248,6 +250,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   a.R = d.R; a.T = d.T; a.S = d.S; a.Hq = d.Hq; a.Hkv = d.Hkv; a.Dh = d.Dh;
   a.max_k = d.max_k < d.S ? d.max_k : d.S;
   a.ps = fast_div(1);
+  a.group = fast_div((uint32_t)(d.Hq / d.Hkv));
   a.c = exp2_scale(d.scale, d.Dh);
   HIPCHECK(launch_attn_ragged(a, p, ws, stream));
   return WAM_OK;

@@ -318,8 +318,8 @@ struct RaggedArgs {
   const int32_t *table, *q_start, *q_len, *k_start, *k_len;  // k_len: kv_len of the paged form
   int64_t table_stride, q_ts, o_ts;
   int64_t page_stride, tok_stride, head_stride;
-  int32_t R, T, Hq, Hkv, Dh, max_k, chunk, n_pages, S;
-  FastDiv ps;
+  int32_t R, T, Hq, Hkv, Dh, max_k, n_pages, S;
+  FastDiv ps, group, chunk;  // page size, query heads per KV head, chunk (d = 0: none)
   float c, v_scale;  // c: softmax scale * log2(e)
 };
 hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws, hipStream_t s);
