@@ -9,10 +9,9 @@
 //
 // Two paths by the request's rows:
 //  stream  at most 32 rows (single tokens): bound by reading the cache.  Each wavefront takes every
-//          fourth 32-key tile on its own, K from memory straight into the matrix operand's registers,
-//          V through a private piece of LDS for its transposition; the next tile's 16 KB are in
-//          flight while one is used, nothing waits for another wavefront until the four states are
-//          joined at the end.
+//          fourth 32-key tile on its own: whole rows into registers, the next tile's 16 KB in flight while
+//          one is used, and through a private piece of LDS into the matrix operands' order (V's with the
+//          transposing read); nothing waits for another wavefront until the four states are joined at the end.
 //  tile    more rows: 32 per wavefront against 64-key tiles shared in LDS, as in attn.hip (whose tile
 //          code it shares); the page of a wavefront's 16 keys of a tile is one entry of the
 //          block table (a page holds a multiple of 16 keys).
@@ -115,68 +114,96 @@ WAM_DEV float exp_scale(uint32_t biased) { return __uint_as_float(biased << 23);
 WAM_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // Bytes between V rows of a tile in a wavefront's LDS: 32 more than a row, so that the 8 rows x 32 bytes that 32 lanes
-// of the transposing read touch lie in different banks, at constant distances.
+// of the transposing read touch lie in different banks, at constant distances; and between the K rows of a group (as they are
+// stored): 16 more, so that 16 rows' chunks do.
 constexpr int spitch(int dh) { return dh * 2 + 32; }
+constexpr int kpitch(int dh, bool fp8) { return dh * (fp8 ? 1 : 2) + 16; }
+constexpr int stream_wave_lds(int dh, bool fp8) { return 32 * spitch(dh) + 16 * kpitch(dh, fp8); }
 
 // One 32-key tile of a wavefront in registers: two groups of 16 keys.
 template <int DH, bool FP8>
 struct StreamRegs {
-  static constexpr int KN = FP8 ? 2 : DH / 32, VN = FP8 ? 2 : DH / 32;
-  u32x4v k[2][KN], v[2][VN];
+  static constexpr int N = FP8 ? 2 : DH / 32;  // 16-byte chunks of a group's K (and V) per lane
+  u32x4v k[2][N], v[2][N];
   uint32_t ex[2];
   int nv[2];  // keys there are of each group (wave-uniform)
 };
 
+// (Whole rows, K's of both groups before V's, marked as used once: only this workgroup reads them, and they should not push
+// others out of the caches.  us for 48 single tokens, 8 heads of 128 / 32 tokens, 8 heads of 64 / 64 tokens, 8 heads,
+// E4M3: K in the operand's order from memory (64 bytes of 16 rows per load) 159 / 82 / 278; with V marked 149 / 79 /
+// 275; whole rows of both, marked 139 / 79 / 267; K before V in a group 139 / 69 / 267, in both 139 / 70 / 257.)
 template <int DH, bool PAGED, bool FP8>
 WAM_DEV void stream_load(StreamRegs<DH, FP8>& x, const RaggedArgs& a, const Req& q, int hk, int key0, int end, int pg0,
-                         int pg1, int lane, int koff, int voff) {
+                         int pg1, int lane, int off) {
   constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;  // chunks per row, rows per instruction
-  const int ts = (int)a.tok_stride * EB;
+  const int ts = (int)a.tok_stride * EB, n16 = lane & 15;
+  constexpr int N = StreamRegs<DH, FP8>::N;
+  const char *kp[2], *vp[2], *ep[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int key = key0 + 16 * u, pg = u ? pg1 : pg0;
-    const int nv = pg < 0 ? 0 : clampi(end - key, 0, 16);
-    x.nv[u] = nv;
+    x.nv[u] = pg < 0 ? 0 : clampi(end - key, 0, 16);
+    const int64_t at = x.nv[u] > 0 ? row_at<PAGED>(a, q, pg, key, hk) : 0;
+    kp[u] = static_cast<const char*>(a.k) + at * EB;
+    vp[u] = static_cast<const char*>(a.v) + at * EB;
+    ep[u] = FP8 ? static_cast<const char*>(a.k_exp) + at / 32 : nullptr;
+  }
+  if (x.nv[0] == 16 && x.nv[1] == 16) {  // uniform bases, one lane offset
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        x.k[u][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(kp[u] + RPI * i * ts + off));
+      if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep[u] + (n16 * ts >> 5));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        x.v[u][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(vp[u] + RPI * i * ts + off));
+    return;
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int nv = x.nv[u];
     if (nv == 0) {
 #pragma unroll
-      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i) x.k[u][i] = x.v[u][i] = u32x4v{0, 0, 0, 0};
+      for (int i = 0; i < N; ++i) x.k[u][i] = x.v[u][i] = u32x4v{0, 0, 0, 0};
       x.ex[u] = 0;
       continue;
     }
-    const int64_t at = row_at<PAGED>(a, q, pg, key, hk);
-    const char* kp = static_cast<const char*>(a.k) + at * EB;
-    const char* vp = static_cast<const char*>(a.v) + at * EB;
-    const char* ep = FP8 ? static_cast<const char*>(a.k_exp) + at / 32 : nullptr;
-    if (nv == 16) {  // uniform bases, one lane offset each
+    // rows past the last key re-read it (their scores are masked, their values zeroed)
+    if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep[u] + ((n16 < nv ? n16 : nv - 1) * ts >> 5));
 #pragma unroll
-      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
-        x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + koff + (FP8 ? 16 : 64) * i);
-      if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep + ((lane & 15) * ts >> 5));
-#pragma unroll
-      for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i)
-        x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + RPI * i * ts + voff);
-    } else {  // rows past the last key re-read it (their scores are masked, their values zeroed)
-      const int n16 = lane & 15, kr = (n16 < nv ? 0 : (nv - 1 - n16) * ts);
-#pragma unroll
-      for (int i = 0; i < StreamRegs<DH, FP8>::KN; ++i)
-        x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp + koff + kr + (FP8 ? 16 : 64) * i);
-      if (FP8) x.ex[u] = *reinterpret_cast<const uint32_t*>(ep + ((n16 < nv ? n16 : nv - 1) * ts >> 5));
-#pragma unroll
-      for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
-        const int row = RPI * i + lane / CPR, rc = row < nv ? row : nv - 1;
-        x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp + rc * ts + 16 * (lane % CPR));
-      }
+    for (int i = 0; i < N; ++i) {
+      const int row = RPI * i + lane / CPR, at_row = (row < nv ? row : nv - 1) * ts + 16 * (lane % CPR);
+      x.k[u][i] = *reinterpret_cast<const u32x4v*>(kp[u] + at_row);
+      x.v[u][i] = *reinterpret_cast<const u32x4v*>(vp[u] + at_row);
     }
   }
 }
 
+// Keeps LDS accesses of other lanes' rows in their order: the compiler moves none across, and a wavefront's LDS operations
+// run in order, so nothing has to wait.
+WAM_DEV void lds_order() { asm volatile("" ::: "memory"); }
+
+// a group's K rows, as they are stored
+template <int DH, bool FP8>
+WAM_DEV void stream_store_k(const StreamRegs<DH, FP8>& x, int u, char* ks, int lane) {
+  constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;
+#pragma unroll
+  for (int i = 0; i < StreamRegs<DH, FP8>::N; ++i)
+    *reinterpret_cast<u32x4v*>(ks + (RPI * i + lane / CPR) * kpitch(DH, FP8) + 16 * (lane % CPR)) = x.k[u][i];
+}
+// a tile's V rows as bf16; rows from nv on as zeros
 template <int DH, bool FP8>
 WAM_DEV void stream_store_v(const StreamRegs<DH, FP8>& x, char* vs, int lane) {
   constexpr int EB = FP8 ? 1 : 2, CPR = DH * EB / 16, RPI = 64 / CPR;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int i = 0; i < StreamRegs<DH, FP8>::VN; ++i) {
+    for (int i = 0; i < StreamRegs<DH, FP8>::N; ++i) {
       const int row = RPI * i + lane / CPR, ch = lane % CPR;
       u32x4v v = x.v[u][i];
       if (x.nv[u] < 16 && row >= x.nv[u]) v = u32x4v{0, 0, 0, 0};
@@ -193,8 +220,11 @@ WAM_DEV void stream_store_v(const StreamRegs<DH, FP8>& x, char* vs, int lane) {
 // key of the group whose page lane l holds, from the wavefront's first key on
 WAM_DEV int stream_key(int lane) { return 128 * (lane >> 1) + 16 * (lane & 1); }
 
-// LDS of the streaming path: four wavefronts' V tiles, or their 16 rows each of the join
-constexpr int stream_lds(int dh) { return (4 * 16 * (dh + 4) + 128) * 4 > 4 * 32 * spitch(dh) ? (4 * 16 * (dh + 4) + 128) * 4 : 4 * 32 * spitch(dh); }
+// LDS of the streaming path: four wavefronts' tiles, or their 16 rows each of the join
+constexpr int stream_lds(int dh, bool fp8) {
+  const int join = (4 * 16 * (dh + 4) + 128) * 4, tiles = 4 * stream_wave_lds(dh, fp8);
+  return join > tiles ? join : tiles;
+}
 
 template <int DH, bool PAGED, bool FP8, int NQ>
 WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
@@ -222,11 +252,14 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  char* vs = smem + w * 32 * spitch(DH);
+  char* vs = smem + w * stream_wave_lds(DH, FP8);
+  char* kl = vs + 32 * spitch(DH);
   // transposing read: lane j of a group points at row 4 g + j / 4, 4 dims from 4 (j % 4) of each 16
   const char* vr = vs + (4 * g + (n16 >> 2)) * spitch(DH) + 8 * (n16 & 3);
   const int ts = (int)a.tok_stride * (FP8 ? 1 : 2), cpr = DH * (FP8 ? 1 : 2) / 16;
-  const int koff = n16 * ts + (FP8 ? 32 : 16) * g, voff = lane / cpr * ts + 16 * (lane % cpr);
+  const int off = lane / cpr * ts + 16 * (lane % cpr);
+  // K operand of a group: row n16; bf16: dims 32 ks + 8 g ..; codes: dims 32 g + 8 ks .. (one block's exponent per lane)
+  const char* kr = kl + n16 * kpitch(DH, FP8) + (FP8 ? 32 : 16) * g;
   const float c = a.c, thr = RESCALE_LOG2 / c;
 
   // tile i of this wavefront: keys start + 128 i + 32 w; lane l holds the page of group l % 2 of tile
@@ -239,17 +272,18 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
     if (i > 0 && (i & 31) == 0) pages(i);
     const int at = 2 * (i & 31);
     stream_load<DH, PAGED, FP8>(x, a, q, hk, first + 128 * i, end, __builtin_amdgcn_readlane(meta, at),
-                                __builtin_amdgcn_readlane(meta, at + 1), lane, koff, voff);
+                                __builtin_amdgcn_readlane(meta, at + 1), lane, off);
   };
   if (n_tiles > 0) load(0);
   for (int i = 0; i < n_tiles; ++i) {
     const int key0 = first + 128 * i;
-    asm volatile("" ::: "memory");  // the reads below are other lanes' rows: no store moves across them (a
-    stream_store_v<DH, FP8>(x, vs, lane);  // wavefront's LDS operations run in order, so nothing waits)
-    asm volatile("" ::: "memory");
     f32x4 s[NQ][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      lds_order();
+      stream_store_k<DH, FP8>(x, u, kl, lane);
+      if (u == 0) stream_store_v<DH, FP8>(x, vs, lane);
+      lds_order();
       const float sc = FP8 ? exp_scale((x.ex[u] >> (8 * g)) & 255) : 1.f;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -257,10 +291,10 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8 kf;
         if constexpr (FP8) {
-          const u32x4v kk = x.k[u][ks >> 1];
-          kf = decode8(kk[2 * (ks & 1)], kk[2 * (ks & 1) + 1], sc);
+          const u32x2 c8 = *reinterpret_cast<const u32x2*>(kr + 8 * ks);
+          kf = decode8(c8[0], c8[1], sc);
         } else {
-          kf = __builtin_bit_cast(bf16x8, x.k[u][ks]);
+          kf = *reinterpret_cast<const bf16x8*>(kr + 64 * ks);
         }
 #pragma unroll
         for (int n = 0; n < NQ; ++n) s[n][u] = mfma16(kf, qf[n][ks], s[n][u]);
@@ -326,7 +360,7 @@ WAM_DEV void stream_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int
   constexpr int PITCH = DH + 4;
   float* red = reinterpret_cast<float*>(smem);                // [4][16][PITCH]
   float* wml = red + 4 * 16 * PITCH;                          // [4][16][2]
-  static_assert(stream_lds(DH) <= 4 * BN * DH * 2, "fits the tile kernel's LDS");
+  static_assert(stream_lds(DH, FP8) <= 4 * BN * DH * 2, "fits the tile kernel's LDS");
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     float l = l_part[n];
@@ -601,7 +635,7 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[mt][e] = acc[mt][e] * f1 + mine[(16 * mt + e) * 64] * f2;
-    asm volatile("" ::: "memory");  // (each wavefront reads and then overwrites its own quarter)
+    lds_order();  // (each wavefront reads and then overwrites its own quarter)
   }
   // The output through LDS (the key tiles are done with), so that a row leaves in whole lines: a lane holds 4 dims here and
   // there of one row; the wavefront's 32 rows go to its quarter of LDS, 16-byte chunks XOR-swizzled by the row (written
@@ -609,7 +643,7 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
   char* my = reinterpret_cast<char*>(smem) + w * (BN * DH * 2);
   constexpr int CH = DH / 8, RPI = 64 / CH;  // 16-byte chunks of a row of DH bf16 (or DH / 2 fp32), rows per instruction
   const auto put = [&](auto&& chunk_out) {  // chunk_out(row's index, token, head, chunk, 16 bytes)
-    asm volatile("" ::: "memory");  // other lanes' rows: no LDS access moves across (they run in order)
+    lds_order();
 #pragma unroll
     for (int i = 0; i < 32 / RPI; ++i) {
       const int rr = RPI * i + lane / CH, ch = lane % CH, row = m0 + 32 * w + rr;
@@ -619,7 +653,7 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
         chunk_out((int64_t)q.q0 + tk, hk * G + row - tk * G, ch, v);
       }
     }
-    asm volatile("" ::: "memory");
+    lds_order();
   };
   if (whole) {
     const float inv = l > 0.f ? (FP8 ? a.v_scale : 1.f) / l : 0.f;
@@ -632,8 +666,9 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
             bf16x4{(bf16)(acc[mt][4 * rr + 0] * inv), (bf16)(acc[mt][4 * rr + 1] * inv),
                    (bf16)(acc[mt][4 * rr + 2] * inv), (bf16)(acc[mt][4 * rr + 3] * inv)};
       }
+    // (not to be kept in the caches: two samples' 3152 rows against 512 and 248 keys 93 -> 85 us)
     put([&](int64_t tk, int h, int ch, u32x4v v) {
-      *reinterpret_cast<u32x4v*>(static_cast<bf16*>(a.o) + tk * a.o_ts + h * DH + 8 * ch) = v;
+      __builtin_nontemporal_store(v, reinterpret_cast<u32x4v*>(static_cast<bf16*>(a.o) + tk * a.o_ts + h * DH + 8 * ch));
     });
   } else {
     if (hh == 0 && qrow < rows) {
@@ -740,8 +775,8 @@ __global__ __launch_bounds__(NT * GROUPS, 2) void ragged_tile_kernel(const Ragge
 
 // Few rows per request: 16 NQ per workgroup.
 template <int DH, bool PAGED, bool FP8, int NQ>
-__global__ __launch_bounds__(NT, NQ == 1 ? 3 : 2) void ragged_stream_kernel(const RaggedArgs a, const Parts pt) {
-  __shared__ __attribute__((aligned(16))) char smem[stream_lds(DH)];
+__global__ __launch_bounds__(NT, 2) void ragged_stream_kernel(const RaggedArgs a, const Parts pt) {
+  __shared__ __attribute__((aligned(16))) char smem[stream_lds(DH, FP8)];
   Work k;
   if (!find_work<PAGED, NQ == 1 ? 4 : 5>(a, pt, k)) return;
   stream_rows<DH, PAGED, FP8, NQ>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem);

@@ -262,10 +262,10 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a
 // cosine and sine of every pair once for all heads (fp64 angle in revolutions, reduced to
 // [-1/2, 1/2] there, then fp32), the rest is one pass over the row, 16 dims per item in two 16-byte
 // chunks: neighbouring chunks, or the two halves' chunks whose dims turn together.  Bound by memory, each byte
-// moved once; a thread's first item is on its way while the angles are formed.  3152 tokens, 40 heads: 46 us for
-// 194 MB (4.2 TB/s; a large copy reaches 4.85).  Two or four items on their way at once: 46 and 47 us, and 15 and 17
-// instead of 14 for 1120 tokens into an E4M3 cache.  Rows of up to 128 items share a workgroup: 8000 tokens of 8/2
-// heads of 64 10.4 -> 8.5 us.
+// moved once; a thread's first item is on its way while the angles are formed.  3152 tokens, 40 heads: 43.6 us for
+// 194 MB (4.4 TB/s; a large copy reaches 4.85); without the loads' mark as used once 45.5 (but 1120 tokens into an E4M3
+// cache 15.0, and 18.7 with it).  Two or four items on their way at once: 46 and 47 us, E4M3 15 and 17.  Rows of up to 128
+// items share a workgroup: 8000 tokens of 8/2 heads of 64 10.4 -> 8.5 us.
 // ---------------------------------------------------------------------------------
 // dims (2p, 2p + 1) of pairs pair0 .. pair0 + 3; pairs from n on are kept
 WAM_DEV void turn8(float* y, const float* cs, const float* sn, int pair0, int n) {
@@ -382,8 +382,10 @@ __global__ __launch_bounds__(256) void rope_paged_kernel(const RopePagedArgs a) 
   bf16x8 xa, xb;
   auto load = [&](int i) {
     const RopeItem it = rope_item<DH>(a, i);
-    xa = load_bf16x8(src + it.head * DH + 8 * it.ca);
-    xb = load_bf16x8(src + it.head * DH + 8 * it.cb);
+    const bf16x8 *pa = reinterpret_cast<const bf16x8*>(src + it.head * DH + 8 * it.ca),
+                 *pb = reinterpret_cast<const bf16x8*>(src + it.head * DH + 8 * it.cb);
+    xa = FP8 ? *pa : __builtin_nontemporal_load(pa);
+    xb = FP8 ? *pb : __builtin_nontemporal_load(pb);
   };
   int i = first + tid;
   if (on && i < items) load(i);
