@@ -527,6 +527,8 @@ typedef struct {
  *      entries within one.
  *   2. The pages that are missing (entries [held, need)) are taken from its top, in the same order; an
  *      entry for which the stack holds no page any more becomes -1 (status[0] counts them).
+ * (Pages for kept tokens that the request does not hold are taken like the new ones, with whatever they
+ * hold.  A page belongs to one request: to share one, its owners keep it out of held and the stack.)
  * Written: block_table entries [held, need); free_list entries [n_free, n_free_out); and
  *   held_out [R]   pages that each request holds now;   n_free_out [1]
  *   q_start [R+1]  first row of each request among the new tokens, packed in request order
@@ -585,13 +587,13 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
  *   chunk = c   j < (floor(p / c) + 1) * c: the chunks up to its own, every chunk c tokens
  *               (Appendix C, Figure 10b; c = 1 is causal attention).
  * A row that sees no key (kv_len = 0, absent pages, p < 0) gives 0.  Query head h reads KV head
- * h / (Hq / Hkv); Hq must be a multiple of Hkv.  scale <= 0 selects 1/sqrt(Dh); Dh 64 or 128.
+ * h / (Hq / Hkv); Hq must be a multiple of Hkv, T * Hq < 2^31.  scale <= 0 selects 1/sqrt(Dh); Dh 64 or 128.
  * q, o: [T] rows of [Hq][Dh] bf16 at their token strides (multiples of 8); o must not overlap q
  * or the cache.  With an FP8 cache K and V are decoded (exactly, to bf16; v_scale is applied in
  * fp32) and q stays bf16.  Rows of the cache that hold no key of a request are not used,
  * whatever they hold; a NaN or infinity in V of a key that only some of a request's rows see may
  * reach its other rows.
- * max_kv bounds kv_len (longer ones are cut); it, R and T choose how the key axis is split, and
+ * max_kv <= 2^30 bounds kv_len (longer ones are cut); it, R and T choose how the key axis is split, and
  * with them the rounding, so results are bitwise the same for the same sizes whatever the
  * device values' order (no atomics).  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes
  * (may be 0: then ws may be NULL), 256-byte aligned; calls that may overlap in time need
@@ -609,7 +611,8 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
 
 /* wam_attn_cross — softmax attention to another sequence's states, of a length per request:
  * every row of request r sees all k_len[r] key rows from row k_start[r] of k and v (0 where there
- * are none).  k, v: [S] rows of [Hkv][Dh] bf16 sharing kv_tok_stride (they may be halves of one buffer).
+ * are none).  k, v: [S] rows of [Hkv][Dh] bf16 sharing kv_tok_stride (they may be halves of one
+ * buffer; the stride is at most 2^25).
  * k_len NULL: k_start holds R + 1 values and request r's keys end where the next one's begin;
  * with k_len, k_start holds R values in any order, and requests may share key rows.  Queries,
  * heads, scale, max_k, workspace and determinism as for wam_attn_paged. */

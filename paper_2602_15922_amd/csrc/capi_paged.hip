@@ -187,6 +187,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   TRY(check_cache(c));
   TRY(check_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv));
   CHECK(d.chunk >= 0, WAM_EINVAL, "chunk=%d is negative", d.chunk);
+  CHECK(std::isfinite(d.scale), WAM_EINVAL, "scale=%g must be finite", (double)d.scale);
   CHECK(d.max_pages >= 0 && d.table_stride >= d.max_pages && d.table_stride <= INT64_MAX / 8 / (d.R + 1), WAM_EINVAL,
         "table_stride=%lld must be >= max_pages=%d >= 0", (long long)d.table_stride, d.max_pages);
   if (d.R == 0 || d.T == 0) return WAM_OK;
@@ -228,6 +229,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   const wam_attn_cross_desc& d = *desc;
   TRY(check_ragged(d.R, d.T, d.Hq, d.Hkv, d.Dh, d.max_k));
   CHECK(d.S >= 0, WAM_EINVAL, "S=%d is negative", d.S);
+  CHECK(std::isfinite(d.scale), WAM_EINVAL, "scale=%g must be finite", (double)d.scale);
   if (d.R == 0 || d.T == 0) return WAM_OK;
   TRY(check_rows(q, o, d.q_tok_stride, d.o_tok_stride, (int64_t)d.Hq * d.Dh));
   if (d.S > 0) {

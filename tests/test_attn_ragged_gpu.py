@@ -73,6 +73,57 @@ def test_absent_pages_are_not_seen(fp8):
             check(run_paged(b, chunk), b.expected(chunk))
 
 
+@pytest.mark.parametrize("n,m,G,Dh,fp8", [(100, 1500, 1, 128, False), (300, 1300, 2, 64, False), (90, 2000, 1, 128, True),
+                                          (40, 900, 3, 128, False), (3, 2500, 4, 128, True), (1, 300, 1, 64, False)])
+def test_one_request_with_holes(n, m, G, Dh, fp8):
+    """One request (the eight-wavefront form where its rows are many): pages missing at the start, in the middle, at the
+    end, and whole parts of the key axis without any."""
+    b = Batch([(n, m)], 2 * G, 2, Dh, 16, seed=n + m, fp8=fp8, tail=1)
+    b.table[0, :2], b.table[0, 30:70], b.table[0, -1], b.table[0, 5] = -1, b.n_pages, -1, 2 ** 30
+    for chunk in (0, 1):
+        log(f"paged one request n={n} m={m} G={G} Dh={Dh} fp8={fp8} chunk={chunk}")
+        check(run_paged(b, chunk), b.expected(chunk), f"chunk={chunk}")
+    b.table[:] = -1
+    got = run_paged(b, 0)
+    assert np.all(got[:n] == 0) and np.all(got[n:] == OLD)
+
+
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(2, 1, 128), (3, 3, 64)])
+def test_many_requests(Hq, Hkv, Dh):
+    """Hundreds of requests, empty ones among them: more than one pass of a wavefront over their starts."""
+    g = np.random.default_rng(Hq)
+    for new in (2, 40):
+        lens = []
+        for _ in range(300):
+            n = int(g.integers(0, new + 1))
+            lens.append((n, n + int(g.integers(0, 60))))
+        b = Batch(lens, Hq, Hkv, Dh, 16, seed=1, tail=70)
+        log(f"paged many requests Hq={Hq} Dh={Dh} new<={new}")
+        check(run_paged(b, 1), b.expected(1))
+
+
+def test_two_calls_at_once():
+    """Two streams, two workspaces, one cache: neither disturbs the other."""
+    import torch
+    import paper_2602_15922_amd as w
+    bs = [Batch([(1, 1500), (2, 900)], 8, 2, 128, 16, seed=41), Batch([(200, 700)], 8, 2, 128, 16, seed=42)]
+    log("paged two streams")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    args, streams = [], [torch.cuda.Stream() for _ in bs]
+    for b in bs:
+        c = b.cache()
+        n = w.wam_attn_paged_workspace_bytes(c, R=len(b.lens), T=b.T, Hq=8, max_kv=b.width * 16)
+        args.append((c, b.q.cuda(), i32(b.table), i32(b.q_start), i32(b.kv_len),
+                     torch.full((b.T, 8, 128), OLD, dtype=torch.bfloat16, device="cuda"), workspace(n)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, s in zip(args, streams):
+            w.wam_attn_paged(*a, chunk=1, stream=s)
+    torch.cuda.synchronize()
+    for a, b in zip(args, bs):
+        check(host(a[5]), b.expected(1))
+
+
 def test_lengths_past_the_table_and_max_kv():
     b = Batch([(4, 100), (1, 40), (50, 90)], 4, 2, 64, 16, seed=2)
     log("paged max_kv")
@@ -193,7 +244,7 @@ def run_cross(q, kv, q_start, k_start, max_k=None, q_len=None, k_len=None):
 @pytest.mark.parametrize("q_lens,k_lens,Hq,Hkv,Dh", [
     ([144, 1, 30], [32, 0, 77], 8, 8, 64), ([1] * 9, [1, 2, 63, 64, 65, 300, 0, 700, 1500], 8, 2, 128),
     ([200, 130], [512, 77], 3, 3, 128), ([1, 0, 2, 129], [5, 3, 33, 640], 20, 4, 64), ([1], [1], 1, 1, 128),
-    ([16, 31], [2000, 31], 4, 1, 128)])
+    ([16, 31], [2000, 31], 4, 1, 128), ([150], [700], 2, 2, 128), ([500], [300], 6, 2, 64)])
 def test_cross(q_lens, k_lens, Hq, Hkv, Dh):
     log(f"cross {q_lens} {k_lens} Hq={Hq} Hkv={Hkv} Dh={Dh}")
     q, kv, qs, ks, S, ref = cross_case(q_lens, k_lens, Hq, Hkv, Dh, 5)

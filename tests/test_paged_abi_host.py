@@ -52,6 +52,8 @@ def test_cache_refusals(bad, status, says):
     (dict(R=-1), {}, 1, b"negative"), (dict(T=-1), {}, 1, b"negative"), (dict(max_kv=-1), {}, 1, b"negative"),
     (dict(Hq=3), {}, 1, b"multiple of Hkv"), (dict(Hq=0), {}, 1, b"Hq"), (dict(Hq=8192), {}, 1, b"Hq"),
     (dict(chunk=-1), {}, 1, b"chunk"), (dict(table_stride=2), {}, 1, b"table_stride"), (dict(max_pages=-1), {}, 1, b"max_pages"),
+    (dict(max_kv=(1 << 30) + 1), {}, 2, b"2^30"), (dict(T=1 << 30), {}, 2, b"2^31"), (dict(R=1 << 30), {}, 2, b"2^31"),
+    (dict(scale=float("inf")), {}, 1, b"scale"), (dict(scale=float("nan")), {}, 1, b"scale"),
     (dict(q_tok_stride=256), {}, 1, b"strides"), (dict(o_tok_stride=516), {}, 1, b"strides"),
     ({}, dict(q=0), 1, b"q is NULL"), ({}, dict(q=4100), 1, b"aligned"), ({}, dict(o=0), 1, b"o is NULL"),
     ({}, dict(table=0), 1, b"block_table is NULL"), ({}, dict(q_start=0), 1, b"q_start is NULL"),
@@ -73,7 +75,8 @@ def test_attn_paged_refusals(bad, ptrs, status, says):
 @pytest.mark.parametrize("bad,ptrs,status,says", [
     (dict(Dh=80), {}, 2, b"Dh=80"), (dict(S=-1), {}, 1, b"S="), (dict(max_k=-2), {}, 1, b"negative"),
     (dict(Hkv=3), {}, 1, b"multiple of Hkv"), (dict(kv_tok_stride=128), {}, 1, b"kv_tok_stride"),
-    (dict(kv_tok_stride=260), {}, 1, b"kv_tok_stride"), ({}, dict(k=0), 1, b"k is NULL"), ({}, dict(v=4104), 1, b"aligned"),
+    (dict(kv_tok_stride=260), {}, 1, b"kv_tok_stride"), (dict(kv_tok_stride=1 << 26), {}, 1, b"kv_tok_stride"),
+    (dict(scale=float("inf")), {}, 1, b"scale"), ({}, dict(k=0), 1, b"k is NULL"), ({}, dict(v=4104), 1, b"aligned"),
     ({}, dict(k_start=0), 1, b"k_start is NULL"), ({}, dict(k_len=2), 1, b"k_len"), ({}, dict(o=8), 1, b"aligned"),
 ])
 def test_attn_cross_refusals(bad, ptrs, status, says):
