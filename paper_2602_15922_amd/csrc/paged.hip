@@ -86,7 +86,7 @@ struct PlanLds {
   alignas(16) int q_at[E * PLAN_NT], take_at[E * PLAN_NT], back_at[E * PLAN_NT];
   int cache[E <= 4 ? E * PLAN_NT : 1], held[E <= 4 ? E * PLAN_NT : 1], need[E <= 4 ? E * PLAN_NT : 1];
   uint32_t wave[3][PLAN_NT / 64];
-  unsigned long long total[3];  // status: new tokens, pages past the width, invalid inputs (may pass 32 bits)
+  uint64_t total[3][PLAN_NT / 64];  // status: new tokens, pages past the width, invalid inputs of each wavefront
 };
 
 // E requests per thread: R <= 256 E.  The first `rows` workgroups fill the new tokens' rows, the last the requests'
@@ -99,7 +99,6 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a
   const bool status = blockIdx.x == gridDim.x - 1;
   uint32_t fresh[E], take[E], back[E], sum[3] = {0, 0, 0};
   uint64_t all_new = 0, all_over = 0, all_bad = 0;
-  if (tid < 3) L.total[tid] = 0;
   const uint32_t most[3] = {(uint32_t)T, 0x7fffffffu, 0x7fffffffu};
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -133,12 +132,16 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a
     if (lane == 0) at[i] = 0;
     if (lane == 63) L.wave[i][w] = incl;
   }
-  __syncthreads();
-  if (status) {  // (integer sums: any order)
-    if (all_new) atomicAdd(&L.total[0], all_new);
-    if (all_over) atomicAdd(&L.total[1], all_over);
-    if (all_bad) atomicAdd(&L.total[2], all_bad);
+  if (status) {
+    const uint64_t total[3] = {all_new, all_over, all_bad};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      // (may pass 32 bits: the low 16 bits and the rest apart)
+      const uint32_t lo = wave_scan((uint32_t)total[i] & 0xffffu, ~0u), hi = wave_scan((uint32_t)(total[i] >> 16), ~0u);
+      if (lane == 63) L.total[i][w] = ((uint64_t)hi << 16) + lo;
+    }
   }
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     uint32_t before = 0;
@@ -196,7 +199,9 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a
       a.kv_len[r] = (int)(kv < INT32_MAX ? kv : INT32_MAX);
     }
     if (tid == 0) {
-      const uint64_t v[3] = {L.total[0], L.total[1], L.total[2]};
+      uint64_t v[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) v[i] = L.total[i][0] + L.total[i][1] + L.total[i][2] + L.total[i][3];
       const uint64_t cut = v[0] - tokens, big = 0x7fffffffu;
       a.q_start[R] = tokens;
       a.n_free_out[0] = (int)(left < 0 ? 0 : (left < a.d.n_pages ? left : a.d.n_pages));
@@ -407,11 +412,11 @@ __global__ __launch_bounds__(256) void rope_paged_kernel(const RopePagedArgs a) 
 }  // namespace
 
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s) {
-  // four rows per thread, a page that changes hands per thread (about those that the new rows need), at most eight
-  // workgroups per CU each; and one
+  // four rows per thread, a page that changes hands per thread (those that the new rows need, and some 16 of each request
+  // that ends or shrinks), at most eight workgroups per CU each; and one
   const auto groups = [](int64_t n) { return (int)(n < 1 ? 1 : (n > 2048 ? 2048 : n)); };
   const int rows = groups(((int64_t)a.d.T + 4 * PLAN_NT - 1) / (4 * PLAN_NT));
-  const int pages = groups(((int64_t)a.d.T / a.d.page_size + a.d.R + PLAN_NT - 1) / PLAN_NT);
+  const int pages = groups(((int64_t)a.d.T / a.d.page_size + 16 * (int64_t)a.d.R + PLAN_NT - 1) / PLAN_NT);
   const dim3 grid((unsigned)(rows + pages + 1)), block(PLAN_NT);
   static_assert(16 * PLAN_NT >= WAM_PLAN_MAX_REQUESTS, "requests per thread");
   if (a.d.R <= PLAN_NT) hipLaunchKernelGGL(page_plan_kernel<1>, grid, block, 0, s, a, rows);
