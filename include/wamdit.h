@@ -593,9 +593,9 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
  * fp32) and q stays bf16.  Rows of the cache that hold no key of a request are not used,
  * whatever they hold; a NaN or infinity in V of a key that only some of a request's rows see may
  * reach its other rows.
- * max_kv <= 2^30 bounds kv_len (longer ones are cut); it, R and T choose how the key axis is split, and
- * with them the rounding, so results are bitwise the same for the same sizes whatever the
- * device values' order (no atomics).  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes
+ * max_kv <= 2^30 bounds kv_len (longer ones are cut); it, R, T and the heads choose how the key axis
+ * is split, and with that the rounding; a call repeated gives the same bits (no atomics), and a
+ * row's do not depend on what the other requests hold.  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes
  * (may be 0: then ws may be NULL), 256-byte aligned; calls that may overlap in time need
  * workspaces of their own. */
 typedef struct {

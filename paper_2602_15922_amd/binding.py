@@ -470,14 +470,18 @@ def make_paged_cache(k, v, k_exp=None, v_scale=0.0) -> wam_paged_cache:
     """One layer's pages: k, v [n_pages, page_size, Hkv, Dh] views (strides taken from the tensors), bf16, or
     uint8 E4M3 codes with k_exp [n_pages, page_size, Hkv] int32 block exponents and v_scale."""
     n_pages, page_size, Hkv, Dh = k.shape
-    if v.shape != k.shape or v.stride() != k.stride():
+    far = [i for i in range(3) if k.shape[i] > 1]  # (the stride of a dimension of one entry says nothing)
+    if v.shape != k.shape or any(v.stride(i) != k.stride(i) for i in far):
         raise ValueError("k and v must share shape and strides")
-    if k.stride(3) != 1:
+    if k.stride(3) != 1 or v.stride(3) != 1:
         raise ValueError("a row's Dh values must be contiguous")
-    if k_exp is not None and any(e * Dh != s for e, s in zip(k_exp.stride(), k.stride())):
+    if k_exp is not None and any(k_exp.stride(i) * Dh != k.stride(i) for i in far):
         raise ValueError("exponent strides must be the code strides / Dh")
-    c = wam_paged_cache(k=_p(k), v=_p(v), k_exp=_p(k_exp), page_stride=k.stride(0), tok_stride=k.stride(1),
-                        head_stride=k.stride(2), n_pages=n_pages, page_size=page_size, Hkv=Hkv, Dh=Dh, v_scale=v_scale)
+    head = k.stride(2) if 2 in far else Dh
+    tok = k.stride(1) if 1 in far else Hkv * head
+    page = k.stride(0) if 0 in far else page_size * max(tok, head)
+    c = wam_paged_cache(k=_p(k), v=_p(v), k_exp=_p(k_exp), page_stride=page, tok_stride=tok, head_stride=head,
+                        n_pages=n_pages, page_size=page_size, Hkv=Hkv, Dh=Dh, v_scale=v_scale)
     c._keep = (k, v, k_exp)
     return c
 

@@ -2,13 +2,14 @@
 // MFMA, fp32 online softmax).
 //
 // The rows of a request and KV head are its tokens times the query heads that share the KV head,
-// token by token; a workgroup owns 128 of them, so a shared head's keys are read once for its
+// token by token; a workgroup owns 128 (16, 32) of them, so a shared head's keys are read once for its
 // whole group.  Row tile x of the launch belongs to the last request r with floor(q_start[r] G / 128)
 // + r <= x: every request has room for its tiles there, the launch needs only T, G and R, and a
 // workgroup finds its request with one pass over q_start.
 //
-// Two paths by the request's rows:
-//  stream  at most 32 rows (single tokens): bound by reading the cache.  Each wavefront takes every
+// Two paths by the request's rows (a kernel for calls whose requests have few on average, 16 or 32 to a workgroup, and
+// one for the others, which streams those that have few all the same):
+//  stream  few rows (single tokens): bound by reading the cache.  Each wavefront takes every
 //          fourth 32-key tile on its own: whole rows into registers, the next tile's 16 KB in flight while
 //          one is used, and through a private piece of LDS into the matrix operands' order (V's with the
 //          transposing read); nothing waits for another wavefront until the four states are joined at the end.
@@ -16,7 +17,7 @@
 //          code it shares); the page of a wavefront's 16 keys of a tile is one entry of the
 //          block table (a page holds a multiple of 16 keys).
 // Where rows are few and keys many the key axis is split over workgroups (ragged_plan.h); the parts
-// are joined in a fixed order by ragged_join_kernel.
+// are joined in a fixed order by a second kernel.
 #include "attn_tile.h"
 #include "kernels.h"
 #include "ragged_plan.h"
@@ -698,14 +699,17 @@ WAM_DEV void tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
 // floor(q_start[r] G / 2^shift) + r
 WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane) {
   if (a.R == 1) return 0;  // (rows before it or past it are none of its)
-  int cnt = 0;
-  for (int b = 0; b < a.R; b += 64) {
-    const int r = b + lane;
+  // 64 requests at a time; of more, first every so-manieth, then those between two (the starts do not fall)
+  int lo = 0, n = a.R;
+  for (;;) {
+    const int step = (n + 63) >> 6, r = lo + lane * step;
     bool in = false;
-    if (r < a.R) in = shift ? (((int64_t)a.q_start[r] * G) >> shift) + r <= x : a.q_start[r] <= x;
-    cnt += __popcll(__ballot(in));
+    if (lane * step < n) in = shift ? (((int64_t)a.q_start[r] * G) >> shift) + r <= x : a.q_start[r] <= x;
+    const int cnt = __popcll(__ballot(in));
+    if (step == 1 || cnt == 0) return lo + cnt - 1;
+    lo += (cnt - 1) * step;
+    n = n - (cnt - 1) * step < step ? n - (cnt - 1) * step : step;
   }
-  return cnt - 1;
 }
 
 // A workgroup's work: its request, KV head, first row, and keys.

@@ -37,27 +37,24 @@ def check(got, ref, what=""):
 MIXED = [(1, 1), (1, 63), (0, 30), (3, 3), (1, 64), (1, 65), (17, 40), (40, 300), (1, 129), (130, 131), (2, 0), (5, 3), (1, 700)]
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh,ps,layout", [
-    (1, 1, 128, 16, "nhd"), (8, 2, 128, 48, "hnd"), (3, 3, 64, 64, "kv"), (16, 1, 64, 16, "nhd"), (5, 5, 128, 32, "kv"),
-    (40, 1, 128, 16, "nhd"), (6, 2, 64, 1024, "hnd")])
-@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,Dh,ps,layout,fp8", [
+    (1, 1, 128, 16, "nhd", False), (8, 2, 128, 48, "hnd", False), (3, 3, 64, 64, "kv", False), (16, 1, 64, 16, "nhd", False),
+    (5, 5, 128, 32, "kv", False), (40, 1, 128, 16, "nhd", False), (6, 2, 64, 1024, "hnd", False), (1, 1, 128, 16, "nhd", True),
+    (8, 2, 128, 48, "hnd", True), (5, 5, 128, 32, "kv", True), (40, 1, 128, 16, "nhd", True)])
 def test_mixed_lengths(Hq, Hkv, Dh, ps, layout, fp8):
-    if fp8 and Dh != 128:
-        pytest.skip("the FP8 cache has heads of 128")
     b = Batch(MIXED, Hq, Hkv, Dh, ps, seed=Hq + ps, fp8=fp8, layout=layout)
     for chunk in (0, 1, 7):
         log(f"paged mixed Hq={Hq} Hkv={Hkv} Dh={Dh} ps={ps} {layout} fp8={fp8} chunk={chunk}")
         check(run_paged(b, chunk), b.expected(chunk), f"chunk={chunk}")
 
 
-@pytest.mark.parametrize("lens,Hq,Hkv,Dh,ps,chunk", [
-    ([(1, n) for n in (1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 49, 127, 128, 255, 256, 257, 511, 513, 1023, 1025)], 4, 1, 128, 16, 1),
-    ([(1, 5000)], 8, 8, 128, 64, 0), ([(1, 3001), (1, 17), (2, 2999)], 5, 5, 64, 16, 1), ([(33, 2100)], 2, 1, 128, 16, 1),
-    ([(128, 1300), (129, 129)], 2, 2, 128, 64, 32), ([(257, 700)], 3, 1, 64, 48, 257), ([(64, 4000)], 1, 1, 128, 32, 0)])
-@pytest.mark.parametrize("fp8", [False, True])
+AXIS = [([(1, n) for n in (1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 49, 127, 128, 255, 256, 257, 511, 513, 1023, 1025)], 4, 1, 128, 16, 1),
+        ([(1, 5000)], 8, 8, 128, 64, 0), ([(1, 3001), (1, 17), (2, 2999)], 5, 5, 64, 16, 1), ([(33, 2100)], 2, 1, 128, 16, 1),
+        ([(128, 1300), (129, 129)], 2, 2, 128, 64, 32), ([(257, 700)], 3, 1, 64, 48, 257), ([(64, 4000)], 1, 1, 128, 32, 0)]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh,ps,chunk,fp8", [(*x, f) for x in AXIS for f in (False, True) if x[3] == 128 or not f])
 def test_key_axis_lengths(lens, Hq, Hkv, Dh, ps, chunk, fp8):
-    if fp8 and Dh != 128:
-        pytest.skip("the FP8 cache has heads of 128")
     b = Batch(lens, Hq, Hkv, Dh, ps, seed=3, fp8=fp8)
     log(f"paged lengths {lens[:3]} Hq={Hq} Hkv={Hkv} Dh={Dh} ps={ps} chunk={chunk} fp8={fp8}")
     check(run_paged(b, chunk), b.expected(chunk))

@@ -170,6 +170,16 @@ def test_binding_checks_tensor_layouts():
         w.make_paged_cache(k, k, k_exp=torch.zeros(4, 16, 4, dtype=torch.int32)[:, :, ::2], v_scale=1.0)
 
 
+def test_binding_takes_any_stride_of_a_single_entry():
+    import torch
+    w, b, L = lib()
+    buf = torch.zeros(16, 128, dtype=torch.bfloat16)
+    k = torch.as_strided(buf, (1, 16, 1, 128), (7, 128, 3, 1))
+    v = torch.as_strided(buf, (1, 16, 1, 128), (0, 128, 0, 1))
+    c = w.make_paged_cache(k, v)
+    assert (c.page_stride, c.tok_stride, c.head_stride) == (16 * 128, 128, 128)
+
+
 def test_reference_rotation_and_chunk_rule():
     pos = np.array([[3, 5], [0, 0], [7, 1]])
     x = np.random.default_rng(0).standard_normal((3, 1, 8))
