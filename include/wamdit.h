@@ -591,8 +591,7 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
  * q, o: [T] rows of [Hq][Dh] bf16 at their token strides (multiples of 8); o must not overlap q
  * or the cache.  With an FP8 cache K and V are decoded (exactly, to bf16; v_scale is applied in
  * fp32) and q stays bf16.  Rows of the cache that hold no key of a request are not used,
- * whatever they hold; a NaN or infinity in V of a key that only some of a request's rows see may
- * reach its other rows.
+ * whatever they hold, and a NaN or infinity of a key reaches the rows that see it and no others.
  * max_kv <= 2^30 bounds kv_len (longer ones are cut); it, R, T and the heads choose how the key axis
  * is split, and with that the rounding; a call repeated gives the same bits (no atomics), and a
  * row's do not depend on what the other requests hold.  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes

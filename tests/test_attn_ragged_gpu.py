@@ -181,6 +181,34 @@ def test_infinite_keys_in_masked_places():
     assert np.all((np.abs(got - o) <= paged_ref.attention_tolerance(a))[:5])
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh,chunk,fp8", [
+    ([(6, 70), (2, 2), (9, 40)], 2, 2, 64, 1, False), ([(6, 70), (3, 129)], 2, 2, 128, 1, False), ([(5, 700), (4, 90)], 8, 2, 128, 1, False),
+    ([(7, 70), (8, 333)], 8, 2, 64, 3, False), ([(6, 170), (5, 64)], 4, 2, 128, 1, True), ([(150, 200), (40, 140), (3, 65)], 4, 2, 128, 1, False),
+    ([(150, 200), (200, 240)], 3, 3, 64, 7, False), ([(100, 190), (65, 65)], 4, 2, 128, 1, True), ([(130, 400)], 1, 1, 128, 1, False),
+    ([(140, 2000)], 2, 1, 128, 32, False), ([(300, 300)], 1, 1, 64, 1, False), ([(90, 1500)], 2, 2, 128, 1, True)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(lens, Hq, Hkv, Dh, chunk, fp8):
+    """V of keys that some rows of a request see and others do not: NaN over a whole row, infinities of both signs in
+    some dims.  The rows that see none are as ever; the others hold what the formula gives, dim by dim."""
+    b = Batch(lens, Hq, Hkv, Dh, 16, seed=sum(n + m for n, m in lens) + Dh, fp8=fp8)
+    for r, (n, m) in enumerate(lens):
+        for back, dims, val in ((1, slice(None), float("nan")), (2, 3, float("inf")), (2, 5, float("-inf")), (3, 3, float("-inf")),
+                                ((n + 1) // 2, 17, float("inf")), ((n + 1) // 2, 18, float("nan")), (n - 1, Dh - 1, float("-inf"))):
+            j = m - max(1, min(back, n - 1))
+            b.v[b.table[r, j // 16], j % 16, :, dims] = 0x7F if fp8 else val
+    log(f"paged values not finite {lens} Hq={Hq} Hkv={Hkv} Dh={Dh} chunk={chunk} fp8={fp8}")
+    with np.errstate(invalid="ignore"):
+        got, (o, a, mine) = run_paged(b, chunk), b.expected(chunk)
+    fin = np.isfinite(o)
+    at = mine[:, None, None] & ~fin
+    assert np.array_equal(np.isnan(got[at]), np.isnan(o[at]))
+    inf = at & np.isinf(o)
+    assert np.array_equal(got[inf], o[inf])
+    ok = mine[:, None, None] & fin
+    assert np.isfinite(got[ok]).all()
+    assert np.all(np.abs(got[ok] - o[ok]) <= paged_ref.attention_tolerance(a)[ok])
+    assert np.all(got[~mine] == OLD)
+
+
 def test_offsets_past_32_bits():
     """Pages whose rows lie more than 4 GiB apart in elements and bytes."""
     import torch
