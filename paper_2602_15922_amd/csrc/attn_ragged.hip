@@ -961,7 +961,8 @@ __global__ __launch_bounds__(256) void ragged_join_few_kernel(const RaggedArgs a
   for (int e = 0; e < PER; ++e) red[w][lane * PER + e] = y[e];
   __syncthreads();
   if (w > 0) return;
-  const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
+  // (a NaN among a part's sums makes the row NaN, also where the part's own weight is 0: all of its scores were NaN)
+  const float inv = sum != 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
   bf16* op = static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + lane * PER;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
@@ -990,7 +991,7 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] += f != 0.f ? f * v[e] : 0.f;
     }
-    const float inv = sum > 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
+    const float inv = sum != 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
     *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + d) =
         bf16x4{(bf16)(y[0] * inv), (bf16)(y[1] * inv), (bf16)(y[2] * inv), (bf16)(y[3] * inv)};
   }

@@ -209,6 +209,29 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them(lens, Hq, Hkv, 
     assert np.all(got[~mine] == OLD)
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh", [([(1, 1), (1, 5000), (1, 90)], 8, 8, 128), ([(3, 3000), (2, 40)], 5, 5, 64),
+                                            ([(100, 4000)], 1, 1, 128), ([(20, 3000)] * 30, 16, 2, 128), ([(150, 400)], 2, 1, 64)])
+def test_keys_that_are_nan_make_the_rows_that_see_them_nan(lens, Hq, Hkv, Dh):
+    """One key, and the first half of a request's keys: whole parts of a split key axis whose scores are all NaN."""
+    for first in (False, True):
+        b = Batch(lens, Hq, Hkv, Dh, 16, seed=21 + Dh)
+        o, a, mine = b.expected(1)
+        ref = np.broadcast_to(mine[:, None, None], o.shape).copy()  # rows that see none
+        for r, (n, m) in enumerate(lens):
+            if r % 2 == 1:
+                continue
+            keys = range(0, (m + 1) // 2) if first else [m - 1]
+            for j in keys:
+                b.k[b.table[r, j // 16], j % 16, Hkv - 1] = float("nan")
+            at = b.q_start[r] + np.arange(n)
+            ref[at if first else at[-1:], Hq - Hq // Hkv:] = False
+        log(f"paged NaN keys {lens[:2]} Hq={Hq} first={first}")
+        got = run_paged(b, 1)
+        assert np.isfinite(got[ref]).all()
+        assert np.isnan(got[mine[:, None, None] & ~ref]).all()
+        assert np.all(np.abs(got[ref] - o[ref]) <= paged_ref.attention_tolerance(a)[ref])
+
+
 def test_offsets_past_32_bits():
     """Pages whose rows lie more than 4 GiB apart in elements and bytes."""
     import torch
