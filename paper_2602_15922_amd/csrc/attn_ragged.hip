@@ -912,6 +912,8 @@ __global__ __launch_bounds__(NT, 2) void ragged_stream_kernel(const RaggedArgs a
 // The join: o = sum_s 2^(c (m_s - m)) o_s / sum_s 2^(c (m_s - m)) l_s over the parts s of a row, in their order.
 // Two forms: for few rows a workgroup for each, its parts over four wavefronts (the chain of loads is what takes the
 // time); for many a thread for four dims of a row, a workgroup for some heads of a token.
+// Every part of a row is written, also where the row sees none of its keys (sum and outputs 0), so a part of weight 0
+// is added like the others: a NaN or an infinity in its outputs reaches the row, as it does within one part.
 template <bool PAGED>
 WAM_DEV int parts_of(const RaggedArgs& a, const Parts& pt, int t, int lane) {  // 0: nothing to join
   const int r = uniform(find_request(a, t, 1, 0, lane));
@@ -952,9 +954,10 @@ __global__ __launch_bounds__(256) void ragged_join_few_kernel(const RaggedArgs a
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float fs = s0 + 4 * j < n ? __shfl(f, s0 + 4 * j, 64) : 0.f;
+      const bool there = s0 + 4 * j < n;
+      const float fs = __shfl(f, there ? s0 + 4 * j : s0, 64);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) y[e] += fs != 0.f ? fs * v[j][e] : 0.f;
+      for (int e = 0; e < PER; ++e) y[e] += there ? fs * v[j][e] : 0.f;
     }
   }
 #pragma unroll
@@ -989,7 +992,7 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
       const f32x4 v = *reinterpret_cast<const f32x4*>(pt.o + (id + s) * DH + d);
       sum += f * l;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += f != 0.f ? f * v[e] : 0.f;
+      for (int e = 0; e < 4; ++e) y[e] += f * v[e];
     }
     const float inv = sum != 0.f ? (FP8 ? a.v_scale : 1.f) / sum : 0.f;
     *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.o) + t * a.o_ts + h * DH + d) =
