@@ -540,8 +540,10 @@ typedef struct {
  *   status [4]     pages missing; pages past the tables' width; new tokens past T;
  *                  invalid inputs (negative lengths, held outside [0, max_pages], n_free
  *                  outside [0, n_pages]: each is cut to its range)
- * held_out and n_free_out must not overlap held and n_free (every workgroup reads those); with
- * the counters kept apart, a call repeated on the same inputs gives the same result.
+ * No written buffer may overlap any other (every workgroup reads the inputs while others store; kv_len is
+ * not cache_len's buffer, nor held_out held's), and such a call is refused; inputs may share one.  Other
+ * buffers may lie between the table's rows.  With the counters kept apart, a call repeated on the same
+ * inputs gives the same result.
  * R <= WAM_PLAN_MAX_REQUESTS, R * max_pages < 2^31.  No workspace; deterministic. */
 #define WAM_PLAN_MAX_REQUESTS 4096
 typedef struct {

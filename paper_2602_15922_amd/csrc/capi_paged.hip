@@ -77,6 +77,21 @@ wam_status check_rows(const void* q, const void* o, int64_t q_ts, int64_t o_ts, 
 float exp2_scale(float scale, int32_t Dh) {
   return (scale > 0.f ? scale : 1.0f / std::sqrt((float)Dh)) * 1.4426950408889634f;
 }
+// A buffer of a call: `rows` rows of `n` ints, `stride` apart.
+struct Ints {
+  const char* name;
+  const int32_t* p;
+  int64_t n, rows, stride;
+  bool written;
+};
+// (b has one row; both are 4-byte aligned, so whole ints count)
+bool overlap(const Ints& a, const Ints& b) {
+  if (!a.p || !b.p || a.n <= 0 || a.rows <= 0 || b.n <= 0) return false;
+  const int64_t d = ((int64_t)reinterpret_cast<uintptr_t>(b.p) - (int64_t)reinterpret_cast<uintptr_t>(a.p)) / 4;
+  // the first of a's rows that ends past b's first int
+  const int64_t r = d < 0 ? 0 : a.rows == 1 ? d >= a.n : d / a.stride + (d % a.stride >= a.n);
+  return r < a.rows && r * a.stride < d + b.n;
+}
 wam_status check_ws(const void* ws, size_t have, size_t need) {
   CHECK(need == 0 || (ws && (reinterpret_cast<uintptr_t>(ws) & 255) == 0 && have >= need), WAM_EWORKSPACE,
         "workspace of %zu bytes (256-byte aligned) needed, got %zu", need, ws ? have : (size_t)0);
@@ -115,8 +130,23 @@ wam_status wam_page_plan(const wam_page_plan_desc* desc, const int32_t* cache_le
   TRY(need_ints(q_start, "q_start"));
   TRY(need_ints(status, "status"));
   TRY(opt_ints(token_pos, "token_pos"));
-  CHECK(n_free_out != n_free && (d.R == 0 || held_out + d.R <= held || held + d.R <= held_out), WAM_EINVAL,
-        "held_out and n_free_out must not overlap held and n_free");
+  // Every workgroup reads the inputs while others store, so nothing written may lie on anything else.
+  const Ints all[] = {{"block_table", block_table, d.max_pages, d.R, d.table_stride, true},
+                      {"free_list", free_list, d.n_pages, 1, 0, true},
+                      {"held_out", held_out, d.R, 1, 0, true},
+                      {"n_free_out", n_free_out, 1, 1, 0, true},
+                      {"q_start", q_start, d.R + 1, 1, 0, true},
+                      {"kv_len", kv_len, d.R, 1, 0, true},
+                      {"slots", slots, d.T, 1, 0, true},
+                      {"token_pos", token_pos, d.T, 1, 0, true},
+                      {"status", status, 4, 1, 0, true},
+                      {"cache_len", cache_len, d.R, 1, 0, false},
+                      {"new_len", new_len, d.R, 1, 0, false},
+                      {"held", held, d.R, 1, 0, false},
+                      {"n_free", n_free, 1, 1, 0, false}};
+  for (const Ints& x : all)
+    for (const Ints& y : all)
+      CHECK(&x >= &y || !x.written || !overlap(x, y), WAM_EINVAL, "%s and %s overlap", x.name, y.name);
   PagePlanArgs a{};
   a.d = d;
   a.ps = fast_div((uint32_t)d.page_size);
