@@ -1,6 +1,7 @@
 // C ABI of the paged KV cache: argument checks and launches of the page plan, the rotary
 // append, and the ragged attentions.
 #include <cmath>
+#include <limits>
 
 #include "capi_check.h"
 #include "kernels.h"
@@ -171,11 +172,16 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
   for (int x = 0; x < d.n_axes; ++x) {
     CHECK(d.pairs[x] >= 0 && d.pairs[x] <= cache->Dh / 2 - a.n, WAM_EINVAL,
           "pairs[%d]=%d: the axes' pairs must be >= 0 and at most Dh/2=%d together", x, d.pairs[x], cache->Dh / 2);
-    // theta^(-i / pairs) by repeated products in fp64 (at most 64: a few units in the last place)
-    const double step = d.pairs[x] ? std::pow(d.theta, -1.0 / d.pairs[x]) : 1.0;
-    double w = 0.15915494309189535;  // 1 / (2 pi)
+    // theta^(-i / pairs) / (2 pi) by repeated products of 64-bit mantissas (2^-64 of the value each, at most 127), rounded to
+    // fp64 once: a position of 2^31 multiplies what is off.  (Products in fp64 were off by up to 33 units in the last
+    // place, 2^-18.4 rad at 2^31 and theta = 1.1.)
+#ifndef __HIP_DEVICE_COMPILE__  // (the device's own long double is not used)
+    static_assert(std::numeric_limits<long double>::digits >= 64, "extended precision");
+#endif
+    const long double step = d.pairs[x] ? std::pow((long double)d.theta, -1.0L / d.pairs[x]) : 1.0L;
+    long double w = 0.15915494309189533576888376337251436L;
     for (int i = 0; i < d.pairs[x]; ++i, w *= step) {
-      a.turns[a.n] = w;
+      a.turns[a.n] = (double)w;
       a.axis[a.n++] = (uint8_t)x;
     }
   }
