@@ -466,49 +466,133 @@ def wam_rope_qkv(qkv, cos_t, sin_t, q_out, k_cache, v_cache, row0, H, Dh, stream
 # ------------------------------------------------------------------------------------------
 # the KV cache in pages
 # ------------------------------------------------------------------------------------------
+# These calls pass addresses on, and lengths and tables are read on the device where nothing can refuse them, so the
+# binding refuses what the addresses cannot say: another type, order, size or device.
+def _need_ints(dev, n, names, *tensors):
+    """int32, contiguous, at least n entries, on device number dev; None passes."""
+    import torch
+    i32 = torch.int32
+    for t in tensors:
+        if t is not None and (t.dtype is not i32 or t.numel() < n or t.get_device() != dev or not t.is_contiguous()):
+            name = names.split()[[x is t for x in tensors].index(True)]
+            raise ValueError(f"{name} must be a contiguous int32 tensor of at least {n} entries on the call's device, "
+                             f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _need_table(dev, t):
+    import torch
+    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.get_device() != dev:
+        raise ValueError(f"block_table must be an int32 tensor [R, max_pages] of contiguous rows on the call's device, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _need_heads(dev, n, H, Dh, names, *tensors):
+    """bf16 [at least n rows, H, Dh], a row's heads contiguous, on device number dev."""
+    import torch
+    for t in tensors:
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[0] < n or shape[1] != H or shape[2] != Dh or
+                stride[2] != 1 or (H > 1 and stride[1] != Dh) or t.get_device() != dev):
+            name = names.split()[[x is t for x in tensors].index(True)]
+            raise ValueError(f"{name} must be a bf16 tensor [{n}, {H}, {Dh}] of contiguous rows on the call's device, "
+                             f"got {t.dtype} {tuple(shape)} strides {stride} on {t.device}")
+
+
+def _need_workspace(dev, ws):
+    """Bytes of the workspace."""
+    if ws is None:
+        return 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the call's device")
+    return ws.numel()
+
+
+def _stream_on(stream, dev):
+    """The stream's handle, which must belong to the tensors' device."""
+    if dev < 0:
+        raise ValueError("the tensors must be on the GPU")
+    import torch
+    at = torch.cuda.current_device() if stream is None else getattr(stream, "device_index", dev)
+    if at != dev:
+        raise ValueError(f"the tensors are on GPU {dev}, the stream is on GPU {at}")
+    return _stream(stream)
+
+
+def _cache_on(cache, dev):
+    if getattr(cache, "_dev", dev) != dev:
+        raise ValueError("the cache and the other tensors must be on one device")
+
+
 def make_paged_cache(k, v, k_exp=None, v_scale=0.0) -> wam_paged_cache:
     """One layer's pages: k, v [n_pages, page_size, Hkv, Dh] views (strides taken from the tensors), bf16, or
     uint8 E4M3 codes with k_exp [n_pages, page_size, Hkv] int32 block exponents and v_scale."""
+    import torch
     n_pages, page_size, Hkv, Dh = k.shape
     far = [i for i in range(3) if k.shape[i] > 1]  # (the stride of a dimension of one entry says nothing)
     if v.shape != k.shape or any(v.stride(i) != k.stride(i) for i in far):
         raise ValueError("k and v must share shape and strides")
     if k.stride(3) != 1 or v.stride(3) != 1:
         raise ValueError("a row's Dh values must be contiguous")
-    if k_exp is not None and any(k_exp.stride(i) * Dh != k.stride(i) for i in far):
-        raise ValueError("exponent strides must be the code strides / Dh")
+    if k_exp is not None and (k_exp.shape != k.shape[:3] or any(k_exp.stride(i) * Dh != k.stride(i) for i in far)):
+        raise ValueError("exponents must have k's shape without Dh, exponent strides must be the code strides / Dh")
+    if k_exp is None and not (k.dtype is v.dtype is torch.bfloat16):
+        raise ValueError(f"k and v must be bf16, or E4M3 codes with k_exp, got {k.dtype} and {v.dtype}")
+    if k_exp is not None and (k.element_size() != 1 or v.element_size() != 1 or k_exp.dtype is not torch.int32):
+        raise ValueError(f"an FP8 cache takes codes of one byte and int32 exponents, got {k.dtype}, {v.dtype} and {k_exp.dtype}")
+    dev = k.get_device()
+    if v.get_device() != dev or (k_exp is not None and k_exp.get_device() != dev):
+        raise ValueError("k, v and k_exp must be on one device")
     head = k.stride(2) if 2 in far else Dh
     tok = k.stride(1) if 1 in far else Hkv * head
     page = k.stride(0) if 0 in far else page_size * max(tok, head)
     c = wam_paged_cache(k=_p(k), v=_p(v), k_exp=_p(k_exp), page_stride=page, tok_stride=tok, head_stride=head,
                         n_pages=n_pages, page_size=page_size, Hkv=Hkv, Dh=Dh, v_scale=v_scale)
-    c._keep = (k, v, k_exp)
+    c._keep, c._dev = (k, v, k_exp), dev
     return c
 
 
 def wam_page_plan(cache_len, new_len, held, n_free, block_table, free_list, held_out, n_free_out, q_start, kv_len,
                   slots, status, page_size: int, token_pos=None, stream=None):
-    """All int32 device tensors: cache_len, new_len, held, held_out, kv_len [R]; n_free, n_free_out [1];
-    block_table [R, max_pages]; free_list [n_pages]; q_start [R + 1]; slots, token_pos [T]; status [4]."""
-    d = wam_page_plan_desc(block_table.shape[0], slots.shape[0], page_size, free_list.shape[0], block_table.shape[1],
-                           block_table.stride(0))
+    """All contiguous int32 device tensors: cache_len, new_len, held, held_out, kv_len [R]; n_free, n_free_out [1];
+    block_table [R, max_pages] (its rows may lie apart); free_list [n_pages]; q_start [R + 1]; slots, token_pos [T];
+    status [4].  Nothing that is written may overlap anything else."""
+    R, width = block_table.shape
+    T, dev = slots.shape[0], block_table.get_device()
+    _need_table(dev, block_table)
+    _need_ints(dev, R, "cache_len new_len held held_out kv_len", cache_len, new_len, held, held_out, kv_len)
+    _need_ints(dev, R + 1, "q_start", q_start)
+    _need_ints(dev, T, "slots token_pos", slots, token_pos)
+    _need_ints(dev, 1, "n_free n_free_out", n_free, n_free_out)
+    _need_ints(dev, 4, "status", status)
+    _need_ints(dev, 0, "free_list", free_list)
+    d = wam_page_plan_desc(R, T, page_size, free_list.shape[0], width, block_table.stride(0))
     _check(lib().wam_page_plan(C.byref(d), _p(cache_len), _p(new_len), _p(held), _p(n_free), _p(block_table),
                                _p(free_list), _p(held_out), _p(n_free_out), _p(q_start), _p(kv_len), _p(slots),
-                               _p(token_pos), _p(status), _stream(stream)))
+                               _p(token_pos), _p(status), _stream_on(stream, dev)))
 
 
 def wam_rope_qkv_paged(cache: wam_paged_cache, qkv, pos, slots, q_out, pairs, halves=False, theta=10000.0,
                        stream=None):
     """qkv [T, (Hq + 2 Hkv) * Dh] bf16 (row stride from the tensor), pos [T, n_axes] int32 contiguous, slots [T]
     int32; q_out [T, Hq, Dh] bf16 (token stride from the tensor) or None; pairs: rotated pairs of each axis."""
-    T, n = qkv.shape[0], len(pairs)
-    if pos.shape[1] != n:
-        raise ValueError("pos must have one column per entry of pairs")
-    d = wam_rope_paged_desc(T=T, Hq=qkv.shape[1] // cache.Dh - 2 * cache.Hkv, n_axes=n, halves=int(halves), theta=theta,
+    import torch
+    (T, width), n, dev = qkv.shape, len(pairs), qkv.get_device()
+    Hq = width // cache.Dh - 2 * cache.Hkv
+    if pos.dim() != 2 or pos.shape[0] < T or pos.shape[1] != n:
+        raise ValueError("pos must have a row per token and one column per entry of pairs")
+    if qkv.dtype is not torch.bfloat16 or qkv.stride(1) != 1 or width % cache.Dh:
+        raise ValueError(f"qkv must be a bf16 tensor of contiguous rows of whole heads of {cache.Dh}, "
+                         f"got {qkv.dtype} {tuple(qkv.shape)} strides {qkv.stride()}")
+    _need_ints(dev, T * n, "pos", pos)
+    _need_ints(dev, T, "slots", slots)
+    if q_out is not None:
+        _need_heads(dev, T, Hq, cache.Dh, "q_out", q_out)
+    _cache_on(cache, dev)
+    d = wam_rope_paged_desc(T=T, Hq=Hq, n_axes=n, halves=int(halves), theta=theta,
                             qkv_tok_stride=qkv.stride(0), q_tok_stride=0 if q_out is None else q_out.stride(0))
     d.pairs[:min(n, WAM_ROPE_MAX_AXES)] = pairs[:WAM_ROPE_MAX_AXES]
     _check(lib().wam_rope_qkv_paged(C.byref(d), C.byref(cache), _p(qkv), _p(pos), _p(slots), _p(q_out),
-                                    _stream(stream)))
+                                    _stream_on(stream, dev)))
 
 
 def wam_attn_paged_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: int, max_kv: int) -> int:
@@ -519,14 +603,19 @@ def wam_attn_paged_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: i
 def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, ws=None, max_kv=None, chunk=0, q_len=None,
                    scale=0.0, stream=None):
     """q, o [T, Hq, Dh] bf16 (token strides from the tensors); block_table [R, max_pages], q_start [R + 1],
-    kv_len and q_len [R] int32; max_kv (default: what the table's width can hold) bounds kv_len; ws a uint8 device
-    tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
-    T, Hq, _ = q.shape
+    kv_len and q_len [R] contiguous int32; max_kv (default: what the table's width can hold) bounds kv_len; ws a uint8
+    device tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
+    (T, Hq, _), dev = q.shape, q.get_device()
     R, width = block_table.shape
+    _need_heads(dev, T, Hq, cache.Dh, "q o", q, o)
+    _need_table(dev, block_table)
+    _need_ints(dev, R + 1, "q_start", q_start)
+    _need_ints(dev, R, "kv_len q_len", kv_len, q_len)
+    _cache_on(cache, dev)
     d = wam_attn_paged_desc(R, T, Hq, width, min(width * cache.page_size, 1 << 30) if max_kv is None else max_kv, chunk,
                             block_table.stride(0), q.stride(0), o.stride(0), scale)
     _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), _p(q), _p(block_table), _p(q_start), _p(q_len), _p(kv_len),
-                                _p(o), _p(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+                                _p(o), _p(ws), _need_workspace(dev, ws), _stream_on(stream, dev)))
 
 
 def wam_attn_cross_workspace_bytes(R: int, T: int, Hq: int, Hkv: int, Dh: int, max_k: int) -> int:
@@ -536,16 +625,22 @@ def wam_attn_cross_workspace_bytes(R: int, T: int, Hq: int, Hkv: int, Dh: int, m
 
 def wam_attn_cross(q, k, v, q_start, k_start, o, ws=None, max_k=None, q_len=None, k_len=None, scale=0.0, stream=None):
     """q, o [T, Hq, Dh] bf16; k, v [S, Hkv, Dh] bf16 views (token strides from the tensors); q_start [R + 1], q_len
-    [R] or None, k_start [R] with k_len [R], or [R + 1] without; max_k (default S) bounds k_len; ws a uint8 device
-    tensor of at least wam_attn_cross_workspace_bytes(R, T, Hq, Hkv, Dh, max_k)."""
-    T, Hq, Dh = q.shape
+    [R] or None, k_start [R] with k_len [R], or [R + 1] without, all contiguous int32; max_k (default S) bounds k_len; ws a
+    uint8 device tensor of at least wam_attn_cross_workspace_bytes(R, T, Hq, Hkv, Dh, max_k)."""
+    (T, Hq, Dh), dev = q.shape, q.get_device()
     S, Hkv, _ = k.shape
+    R = q_start.shape[0] - 1
+    _need_heads(dev, T, Hq, Dh, "q o", q, o)
+    _need_heads(dev, S, Hkv, Dh, "k v", k, v)
     if v.stride(0) != k.stride(0):
         raise ValueError("k and v must share the token stride")
-    d = wam_attn_cross_desc(q_start.shape[0] - 1, T, S, Hq, Hkv, Dh, S if max_k is None else max_k, q.stride(0),
+    _need_ints(dev, R + 1, "q_start", q_start)
+    _need_ints(dev, R, "q_len k_len", q_len, k_len)
+    _need_ints(dev, R if k_len is not None else R + 1, "k_start", k_start)
+    d = wam_attn_cross_desc(R, T, S, Hq, Hkv, Dh, S if max_k is None else max_k, q.stride(0),
                             k.stride(0), o.stride(0), scale)
     _check(lib().wam_attn_cross(C.byref(d), _p(q), _p(k), _p(v), _p(q_start), _p(q_len), _p(k_start), _p(k_len), _p(o),
-                                _p(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+                                _p(ws), _need_workspace(dev, ws), _stream_on(stream, dev)))
 
 
 def make_dims(d, H, Dh, ffn, n_layers, latent_ch=16, act_dim=16, text_dim=4096, freq_dim=256, eps=1e-6):
