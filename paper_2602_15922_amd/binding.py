@@ -2,13 +2,15 @@
 
 Every function here has the name of the C entry point it wraps, takes torch tensors
 (device memory) and plain Python values, checks nothing the library does not check
-itself, and raises ``WamError`` on a non-OK status.  Kernels are launched on torch's
+itself (but the type, order, size and device of the paged operators' tensors, which their
+addresses do not say), and raises ``WamError`` on a non-OK status.  Kernels are launched on torch's
 current stream unless a stream is given.  There is no fallback: if the shared library
 is missing, loading raises.
 """
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -467,55 +469,75 @@ def wam_rope_qkv(qkv, cos_t, sin_t, q_out, k_cache, v_cache, row0, H, Dh, stream
 # the KV cache in pages
 # ------------------------------------------------------------------------------------------
 # These calls pass addresses on, and lengths and tables are read on the device where nothing can refuse them, so the
-# binding refuses what the addresses cannot say: another type, order, size or device.
-def _need_ints(dev, n, names, *tensors):
-    """int32, contiguous, at least n entries, on device number dev; None passes."""
-    import torch
-    i32 = torch.int32
-    for t in tensors:
-        if t is not None and (t.dtype is not i32 or t.numel() < n or t.get_device() != dev or not t.is_contiguous()):
-            name = names.split()[[x is t for x in tensors].index(True)]
-            raise ValueError(f"{name} must be a contiguous int32 tensor of at least {n} entries on the call's device, "
-                             f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+# binding refuses what the addresses cannot say: another type, order, size or device.  (A call of a dozen tensors may take
+# as long as its kernel: tensors are checked together, without a Python call or a loop's turn for each.)
+_of_tensor = _of_device = None
 
 
-def _need_table(dev, t):
-    import torch
-    if t.dtype is not torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.get_device() != dev:
-        raise ValueError(f"block_table must be an int32 tensor [R, max_pages] of contiguous rows on the call's device, "
-                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+def _tensor_methods():
+    global _of_tensor, _of_device
+    if _of_tensor is None:
+        import torch
+        x = torch.Tensor
+        # (the raw handle, as in _stream)
+        _of_device = (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _of_tensor = (torch.int32, torch.bfloat16, x.dtype.__get__, x.get_device, x.is_contiguous, x.numel, x.data_ptr)
+    return _of_tensor
 
 
-def _need_heads(dev, n, H, Dh, names, *tensors):
-    """bf16 [at least n rows, H, Dh], a row's heads contiguous, on device number dev."""
-    import torch
-    for t in tensors:
-        shape, stride = t.shape, t.stride()
-        if (t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[0] < n or shape[1] != H or shape[2] != Dh or
-                stride[2] != 1 or (H > 1 and stride[1] != Dh) or t.get_device() != dev):
-            name = names.split()[[x is t for x in tensors].index(True)]
-            raise ValueError(f"{name} must be a bf16 tensor [{n}, {H}, {Dh}] of contiguous rows on the call's device, "
-                             f"got {t.dtype} {tuple(shape)} strides {stride} on {t.device}")
+def _got(t):
+    return f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}"
 
 
-def _need_workspace(dev, ws):
-    """Bytes of the workspace."""
+def _ints(dev, names, sizes, tensors):
+    """Addresses of tensors that must be int32, contiguous, of at least `sizes` entries, on device number dev."""
+    i32, _, dtype, device, contiguous, numel, data_ptr = _of_tensor or _tensor_methods()
+    if not (set(map(dtype, tensors)) == {i32} and set(map(device, tensors)) == {dev} and
+            all(map(contiguous, tensors)) and all(map(operator.ge, map(numel, tensors), sizes))):
+        for name, n, t in zip(names.split(), sizes, tensors):
+            if t.dtype is not i32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
+                raise ValueError(f"{name} must be a contiguous int32 tensor of at least {n} entries on the call's device, "
+                                 + _got(t))
+    return map(data_ptr, tensors)
+
+
+def _table(dev, t):
+    """Address and row stride of a block table."""
+    i32 = (_of_tensor or _tensor_methods())[0]
+    stride = t.stride()
+    if t.dtype is not i32 or len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1) or t.get_device() != dev:
+        raise ValueError("block_table must be an int32 tensor [R, max_pages] of contiguous rows on the call's device, " + _got(t))
+    return t.data_ptr(), stride[0]
+
+
+def _heads(dev, name, t, n, H, Dh):
+    """Address and token stride of a bf16 tensor [at least n rows, H, Dh], a row's heads contiguous, on device number dev."""
+    bf16 = (_of_tensor or _tensor_methods())[1]
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is not bf16 or t.get_device() != dev or len(shape) != 3 or shape[0] < n or shape[1] != H or shape[2] != Dh
+            or stride[2] != 1 or (stride[1] != Dh and H > 1)):
+        raise ValueError(f"{name} must be a bf16 tensor [{n}, {H}, {Dh}] of contiguous rows on the call's device, " + _got(t))
+    return t.data_ptr(), stride[0]
+
+
+def _workspace(dev, ws):
+    """Address and bytes."""
     if ws is None:
-        return 0
+        return None, 0
     if ws.get_device() != dev or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous tensor on the call's device")
-    return ws.numel()
+        raise ValueError("ws must be a contiguous tensor on the call's device, " + _got(ws))
+    return ws.data_ptr(), ws.numel()
 
 
 def _stream_on(stream, dev):
     """The stream's handle, which must belong to the tensors' device."""
     if dev < 0:
         raise ValueError("the tensors must be on the GPU")
-    import torch
-    at = torch.cuda.current_device() if stream is None else getattr(stream, "device_index", dev)
+    current, raw_stream = _of_device
+    at = current() if stream is None else getattr(stream, "device_index", dev)
     if at != dev:
         raise ValueError(f"the tensors are on GPU {dev}, the stream is on GPU {at}")
-    return _stream(stream)
+    return raw_stream(dev) if stream is None else stream.cuda_stream
 
 
 def _cache_on(cache, dev):
@@ -556,43 +578,37 @@ def wam_page_plan(cache_len, new_len, held, n_free, block_table, free_list, held
     """All contiguous int32 device tensors: cache_len, new_len, held, held_out, kv_len [R]; n_free, n_free_out [1];
     block_table [R, max_pages] (its rows may lie apart); free_list [n_pages]; q_start [R + 1]; slots, token_pos [T];
     status [4].  Nothing that is written may overlap anything else."""
-    R, width = block_table.shape
-    T, dev = slots.shape[0], block_table.get_device()
-    _need_table(dev, block_table)
-    _need_ints(dev, R, "cache_len new_len held held_out kv_len", cache_len, new_len, held, held_out, kv_len)
-    _need_ints(dev, R + 1, "q_start", q_start)
-    _need_ints(dev, T, "slots token_pos", slots, token_pos)
-    _need_ints(dev, 1, "n_free n_free_out", n_free, n_free_out)
-    _need_ints(dev, 4, "status", status)
-    _need_ints(dev, 0, "free_list", free_list)
-    d = wam_page_plan_desc(R, T, page_size, free_list.shape[0], width, block_table.stride(0))
-    _check(lib().wam_page_plan(C.byref(d), _p(cache_len), _p(new_len), _p(held), _p(n_free), _p(block_table),
-                               _p(free_list), _p(held_out), _p(n_free_out), _p(q_start), _p(kv_len), _p(slots),
-                               _p(token_pos), _p(status), _stream_on(stream, dev)))
+    (R, width), T, dev = block_table.shape, slots.shape[0], block_table.get_device()
+    table, stride = _table(dev, block_table)
+    names, sizes = "cache_len new_len held n_free free_list held_out n_free_out q_start kv_len slots status", \
+        (R, R, R, 1, 0, R, 1, R + 1, R, T, 4)
+    ints = cache_len, new_len, held, n_free, free_list, held_out, n_free_out, q_start, kv_len, slots, status
+    if token_pos is not None:
+        names, sizes, ints = names + " token_pos", sizes + (T,), ints + (token_pos,)
+    cache_len, new_len, held, n_free, stack, held_out, n_free_out, q_start, kv_len, slots, status, *pos = \
+        _ints(dev, names, sizes, ints)
+    d = wam_page_plan_desc(R, T, page_size, free_list.shape[0], width, stride)
+    _check(lib().wam_page_plan(C.byref(d), cache_len, new_len, held, n_free, table, stack, held_out, n_free_out, q_start,
+                               kv_len, slots, pos[0] if pos else None, status, _stream_on(stream, dev)))
 
 
 def wam_rope_qkv_paged(cache: wam_paged_cache, qkv, pos, slots, q_out, pairs, halves=False, theta=10000.0,
                        stream=None):
     """qkv [T, (Hq + 2 Hkv) * Dh] bf16 (row stride from the tensor), pos [T, n_axes] int32 contiguous, slots [T]
     int32; q_out [T, Hq, Dh] bf16 (token stride from the tensor) or None; pairs: rotated pairs of each axis."""
-    import torch
-    (T, width), n, dev = qkv.shape, len(pairs), qkv.get_device()
+    bf16 = (_of_tensor or _tensor_methods())[1]
+    (T, width), n, dev, stride = qkv.shape, len(pairs), qkv.get_device(), qkv.stride()
     Hq = width // cache.Dh - 2 * cache.Hkv
     if pos.dim() != 2 or pos.shape[0] < T or pos.shape[1] != n:
         raise ValueError("pos must have a row per token and one column per entry of pairs")
-    if qkv.dtype is not torch.bfloat16 or qkv.stride(1) != 1 or width % cache.Dh:
-        raise ValueError(f"qkv must be a bf16 tensor of contiguous rows of whole heads of {cache.Dh}, "
-                         f"got {qkv.dtype} {tuple(qkv.shape)} strides {qkv.stride()}")
-    _need_ints(dev, T * n, "pos", pos)
-    _need_ints(dev, T, "slots", slots)
-    if q_out is not None:
-        _need_heads(dev, T, Hq, cache.Dh, "q_out", q_out)
+    if qkv.dtype is not bf16 or stride[1] != 1 or width % cache.Dh:
+        raise ValueError(f"qkv must be a bf16 tensor of contiguous rows of whole heads of {cache.Dh}, " + _got(qkv))
+    pos, slots = _ints(dev, "pos slots", (T * n, T), (pos, slots))
+    q, q_stride = (None, 0) if q_out is None else _heads(dev, "q_out", q_out, T, Hq, cache.Dh)
     _cache_on(cache, dev)
-    d = wam_rope_paged_desc(T=T, Hq=Hq, n_axes=n, halves=int(halves), theta=theta,
-                            qkv_tok_stride=qkv.stride(0), q_tok_stride=0 if q_out is None else q_out.stride(0))
+    d = wam_rope_paged_desc(T=T, Hq=Hq, n_axes=n, halves=int(halves), theta=theta, qkv_tok_stride=stride[0], q_tok_stride=q_stride)
     d.pairs[:min(n, WAM_ROPE_MAX_AXES)] = pairs[:WAM_ROPE_MAX_AXES]
-    _check(lib().wam_rope_qkv_paged(C.byref(d), C.byref(cache), _p(qkv), _p(pos), _p(slots), _p(q_out),
-                                    _stream_on(stream, dev)))
+    _check(lib().wam_rope_qkv_paged(C.byref(d), C.byref(cache), qkv.data_ptr(), pos, slots, q, _stream_on(stream, dev)))
 
 
 def wam_attn_paged_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: int, max_kv: int) -> int:
@@ -605,17 +621,19 @@ def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, w
     """q, o [T, Hq, Dh] bf16 (token strides from the tensors); block_table [R, max_pages], q_start [R + 1],
     kv_len and q_len [R] contiguous int32; max_kv (default: what the table's width can hold) bounds kv_len; ws a uint8
     device tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
-    (T, Hq, _), dev = q.shape, q.get_device()
-    R, width = block_table.shape
-    _need_heads(dev, T, Hq, cache.Dh, "q o", q, o)
-    _need_table(dev, block_table)
-    _need_ints(dev, R + 1, "q_start", q_start)
-    _need_ints(dev, R, "kv_len q_len", kv_len, q_len)
+    (T, Hq, _), dev, (R, width), Dh = q.shape, q.get_device(), block_table.shape, cache.Dh
+    qp, q_stride = _heads(dev, "q", q, T, Hq, Dh)
+    op, o_stride = _heads(dev, "o", o, T, Hq, Dh)
+    table, stride = _table(dev, block_table)
+    if q_len is None:
+        q_start, kv_len = _ints(dev, "q_start kv_len", (R + 1, R), (q_start, kv_len))
+    else:
+        q_start, kv_len, q_len = _ints(dev, "q_start kv_len q_len", (R + 1, R, R), (q_start, kv_len, q_len))
     _cache_on(cache, dev)
     d = wam_attn_paged_desc(R, T, Hq, width, min(width * cache.page_size, 1 << 30) if max_kv is None else max_kv, chunk,
-                            block_table.stride(0), q.stride(0), o.stride(0), scale)
-    _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), _p(q), _p(block_table), _p(q_start), _p(q_len), _p(kv_len),
-                                _p(o), _p(ws), _need_workspace(dev, ws), _stream_on(stream, dev)))
+                            stride, q_stride, o_stride, scale)
+    _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), qp, table, q_start, q_len, kv_len, op, *_workspace(dev, ws),
+                                _stream_on(stream, dev)))
 
 
 def wam_attn_cross_workspace_bytes(R: int, T: int, Hq: int, Hkv: int, Dh: int, max_k: int) -> int:
@@ -627,20 +645,21 @@ def wam_attn_cross(q, k, v, q_start, k_start, o, ws=None, max_k=None, q_len=None
     """q, o [T, Hq, Dh] bf16; k, v [S, Hkv, Dh] bf16 views (token strides from the tensors); q_start [R + 1], q_len
     [R] or None, k_start [R] with k_len [R], or [R + 1] without, all contiguous int32; max_k (default S) bounds k_len; ws a
     uint8 device tensor of at least wam_attn_cross_workspace_bytes(R, T, Hq, Hkv, Dh, max_k)."""
-    (T, Hq, Dh), dev = q.shape, q.get_device()
-    S, Hkv, _ = k.shape
-    R = q_start.shape[0] - 1
-    _need_heads(dev, T, Hq, Dh, "q o", q, o)
-    _need_heads(dev, S, Hkv, Dh, "k v", k, v)
-    if v.stride(0) != k.stride(0):
+    (T, Hq, Dh), dev, (S, Hkv, _), R = q.shape, q.get_device(), k.shape, q_start.shape[0] - 1
+    qp, q_stride = _heads(dev, "q", q, T, Hq, Dh)
+    op, o_stride = _heads(dev, "o", o, T, Hq, Dh)
+    kp, kv_stride = _heads(dev, "k", k, S, Hkv, Dh)
+    vp, v_stride = _heads(dev, "v", v, S, Hkv, Dh)
+    if v_stride != kv_stride:
         raise ValueError("k and v must share the token stride")
-    _need_ints(dev, R + 1, "q_start", q_start)
-    _need_ints(dev, R, "q_len k_len", q_len, k_len)
-    _need_ints(dev, R if k_len is not None else R + 1, "k_start", k_start)
-    d = wam_attn_cross_desc(R, T, S, Hq, Hkv, Dh, S if max_k is None else max_k, q.stride(0),
-                            k.stride(0), o.stride(0), scale)
-    _check(lib().wam_attn_cross(C.byref(d), _p(q), _p(k), _p(v), _p(q_start), _p(q_len), _p(k_start), _p(k_len), _p(o),
-                                _p(ws), _need_workspace(dev, ws), _stream_on(stream, dev)))
+    names, sizes, ints = "q_start k_start", (R + 1, R + (k_len is None)), (q_start, k_start)
+    for name, t in (("q_len", q_len), ("k_len", k_len)):
+        if t is not None:
+            names, sizes, ints = f"{names} {name}", sizes + (R,), ints + (t,)
+    q_start, k_start, *lens = _ints(dev, names, sizes, ints)
+    d = wam_attn_cross_desc(R, T, S, Hq, Hkv, Dh, S if max_k is None else max_k, q_stride, kv_stride, o_stride, scale)
+    _check(lib().wam_attn_cross(C.byref(d), qp, kp, vp, q_start, None if q_len is None else lens[0], k_start,
+                                None if k_len is None else lens[-1], op, *_workspace(dev, ws), _stream_on(stream, dev)))
 
 
 def make_dims(d, H, Dh, ffn, n_layers, latent_ch=16, act_dim=16, text_dim=4096, freq_dim=256, eps=1e-6):
