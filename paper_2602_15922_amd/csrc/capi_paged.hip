@@ -75,8 +75,14 @@ wam_status check_rows(const void* q, const void* o, int64_t q_ts, int64_t o_ts, 
         "q and o token strides must be multiples of 8, >= Hq*Dh=%lld", (long long)hd);
   return WAM_OK;
 }
+// the factor of the scores in the exponent of 2
 float exp2_scale(float scale, int32_t Dh) {
   return (scale > 0.f ? scale : 1.0f / std::sqrt((float)Dh)) * 1.4426950408889634f;
+}
+wam_status check_scale(float scale, int32_t Dh) {
+  CHECK(std::isfinite(scale) && std::isfinite(exp2_scale(scale, Dh)), WAM_EINVAL, "scale=%g (times log2(e)) must be finite",
+        (double)scale);
+  return WAM_OK;
 }
 // A buffer of a call: `rows` rows of `n` ints, `stride` apart.
 struct Ints {
@@ -223,7 +229,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   TRY(check_cache(c));
   TRY(check_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv));
   CHECK(d.chunk >= 0, WAM_EINVAL, "chunk=%d is negative", d.chunk);
-  CHECK(std::isfinite(d.scale), WAM_EINVAL, "scale=%g must be finite", (double)d.scale);
+  TRY(check_scale(d.scale, c.Dh));
   CHECK(d.max_pages >= 0 && d.table_stride >= d.max_pages && d.table_stride <= INT64_MAX / 8 / (d.R + 1), WAM_EINVAL,
         "table_stride=%lld must be >= max_pages=%d >= 0", (long long)d.table_stride, d.max_pages);
   if (d.R == 0 || d.T == 0) return WAM_OK;
@@ -265,7 +271,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   const wam_attn_cross_desc& d = *desc;
   TRY(check_ragged(d.R, d.T, d.Hq, d.Hkv, d.Dh, d.max_k));
   CHECK(d.S >= 0, WAM_EINVAL, "S=%d is negative", d.S);
-  CHECK(std::isfinite(d.scale), WAM_EINVAL, "scale=%g must be finite", (double)d.scale);
+  TRY(check_scale(d.scale, d.Dh));
   if (d.R == 0 || d.T == 0) return WAM_OK;
   TRY(check_rows(q, o, d.q_tok_stride, d.o_tok_stride, (int64_t)d.Hq * d.Dh));
   if (d.S > 0) {
