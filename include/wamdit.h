@@ -498,6 +498,8 @@ wam_status wam_denoise_chunk(const wam_model* m, const wam_step_io* io, const wa
  *   cut to the T (S) rows that the call names, keys to max_kv (max_k) and to the table's
  *   width, and a page id outside [0, n_pages) is an absent page, whose keys no query sees.
  *   So no value in them makes a kernel leave the caller's buffers.
+ * Sizes        A call whose launch would have 2^32 threads (rotary append: 64 to 256 per token,
+ *   attentions: 256 per row tile, part and KV head) is WAM_EUNSUPPORTED.
  *
  * wam_paged_cache
  *   k, v       [n_pages][page_size][Hkv][Dh] bf16, row (page, token, head) at page *

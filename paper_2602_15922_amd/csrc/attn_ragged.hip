@@ -1001,12 +1001,11 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
 }
 
 template <int DH, bool PAGED, bool FP8>
-hipError_t launch(const RaggedArgs& a, const Parts& pt, int rows, int groups, hipStream_t s) {
-  const int64_t parts = (int64_t)pt.tiles * pt.splits;
-  const dim3 grid((unsigned)((rows == RAGGED_ROWS ? parts : (parts + 7) / 8 * 8) * a.Hkv)), block(NT);
-  if (rows == 16) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
-  else if (rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 2>), grid, block, 0, s, a, pt);
-  else if (groups == 1) hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
+hipError_t launch(const RaggedArgs& a, const Parts& pt, const RaggedPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)ragged_blocks(p, a.R, a.T, a.Hq, a.Hkv)), block(NT);
+  if (p.rows == 16) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
+  else if (p.rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, PAGED, FP8, 2>), grid, block, 0, s, a, pt);
+  else if (p.groups == 1) hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8, 1>), grid, block, 0, s, a, pt);
   else hipLaunchKernelGGL((ragged_tile_kernel<DH, PAGED, FP8, 2>), grid, dim3(2 * NT), 0, s, a, pt);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pt.splits == 1) return e;
@@ -1031,10 +1030,10 @@ hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws
   pt.by_tiles = fast_div(pt.tiles);
   pt.by_heads = fast_div(a.Hkv);
   if (a.table) {
-    if (a.k_exp) return launch<128, true, true>(a, pt, p.rows, p.groups, s);
-    return a.Dh == 128 ? launch<128, true, false>(a, pt, p.rows, p.groups, s) : launch<64, true, false>(a, pt, p.rows, p.groups, s);
+    if (a.k_exp) return launch<128, true, true>(a, pt, p, s);
+    return a.Dh == 128 ? launch<128, true, false>(a, pt, p, s) : launch<64, true, false>(a, pt, p, s);
   }
-  return a.Dh == 128 ? launch<128, false, false>(a, pt, p.rows, p.groups, s) : launch<64, false, false>(a, pt, p.rows, p.groups, s);
+  return a.Dh == 128 ? launch<128, false, false>(a, pt, p, s) : launch<64, false, false>(a, pt, p, s);
 }
 
 }  // namespace wam

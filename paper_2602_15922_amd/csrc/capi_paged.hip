@@ -68,6 +68,12 @@ wam_status check_ragged(int32_t R, int32_t T, int32_t Hq, int32_t Hkv, int32_t D
         WAM_EUNSUPPORTED, "T * Hq and (R + T * Hq / Hkv / 16) * Hkv * 64 must stay below 2^31");
   return WAM_OK;
 }
+// (a launch's threads are counted in 32 bits)
+wam_status check_launch(int64_t threads) {
+  CHECK(threads <= UINT32_MAX, WAM_EUNSUPPORTED, "%lld threads: more than one launch has (2^32); split the call",
+        (long long)threads);
+  return WAM_OK;
+}
 wam_status check_rows(const void* q, const void* o, int64_t q_ts, int64_t o_ts, int64_t hd) {
   TRY(need_ptr(q, "q"));
   TRY(need_ptr(o, "o"));
@@ -205,6 +211,7 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
         "qkv_tok_stride must be a multiple of 8, >= (Hq + 2 Hkv) * Dh=%lld", (long long)width);
   CHECK(!q_out || (d.q_tok_stride >= (int64_t)d.Hq * cache->Dh && d.q_tok_stride % 8 == 0), WAM_EINVAL,
         "q_tok_stride must be a multiple of 8, >= Hq * Dh");
+  TRY(check_launch((int64_t)d.T * rope_threads(d.Hq, cache->Hkv, cache->Dh) + 255));
   a.c = *cache;
   a.ps = fast_div((uint32_t)cache->page_size);
   a.T = d.T; a.Hq = d.Hq; a.n_axes = d.n_axes; a.halves = d.halves;
@@ -240,6 +247,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
   const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
   TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
+  TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, c.Hkv) * 256 * p.groups));
   RaggedArgs a{};
   a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
   // (a table without columns is never read: no key is below max_k = 0; its address only says "paged")
@@ -287,6 +295,7 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   TRY(opt_ints(k_len, "k_len"));
   const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, d.Hkv, d.Dh, d.max_k);
   TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, d.Dh)));
+  TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, d.Hkv) * 256 * p.groups));
   RaggedArgs a{};
   a.q = q; a.k = k; a.v = v; a.o = o;
   a.q_start = q_start; a.q_len = q_len; a.k_start = k_start; a.k_len = k_len;

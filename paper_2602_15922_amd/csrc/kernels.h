@@ -309,6 +309,11 @@ struct RopePagedArgs {
   double turns[64];   // revolutions per position of each pair
   uint8_t axis[64];
 };
+// threads of a token: 64 or 128 where a row has no more items of 16 dims
+inline int rope_threads(int64_t Hq, int64_t Hkv, int64_t Dh) {
+  const int64_t items = (Hq + 2 * Hkv) * (Dh / 16);
+  return items <= 64 ? 64 : items <= 128 ? 128 : 256;
+}
 hipError_t launch_rope_paged(const RopePagedArgs& a, hipStream_t s);
 
 // Ragged attention over pages (table set) or over rows of packed states (table NULL).

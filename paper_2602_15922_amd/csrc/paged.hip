@@ -427,7 +427,7 @@ hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t s) {
 
 template <int DH, bool FP8>
 static void launch_rope(const RopePagedArgs& a, hipStream_t s) {
-  const int items = (a.Hq + 2 * a.c.Hkv) * (DH / 16), tpt = items <= 64 ? 64 : items <= 128 ? 128 : 256;
+  const int tpt = rope_threads(a.Hq, a.c.Hkv, DH);
   const dim3 grid((unsigned)(((int64_t)a.T * tpt + 255) / 256)), block(256);
   if (tpt == 64) hipLaunchKernelGGL((rope_paged_kernel<DH, FP8, 64>), grid, block, 0, s, a);
   else if (tpt == 128) hipLaunchKernelGGL((rope_paged_kernel<DH, FP8, 128>), grid, block, 0, s, a);

@@ -66,6 +66,13 @@ inline int64_t ragged_tiles(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int r
   return (T * (Hq / Hkv) + rows - 1) / rows + R - 1;
 }
 
+// Workgroups of the launch (256 threads per group of four wavefronts): one per row tile, part and KV head; of the streaming
+// kernel, row tiles and parts in eights, one to each XCD.
+inline int64_t ragged_blocks(const RaggedPlan& p, int64_t R, int64_t T, int64_t Hq, int64_t Hkv) {
+  const int64_t parts = ragged_tiles(R, T, Hq, Hkv, p.rows) * p.splits;
+  return (p.rows == RAGGED_ROWS ? parts : (parts + 7) / 8 * 8) * Hkv;
+}
+
 // Workspace: per row and split the reference and the sum (8 bytes), then Dh partial outputs.
 inline size_t ragged_ml_bytes(const RaggedPlan& p, int64_t T, int64_t Hq) {
   return ((size_t)T * Hq * p.splits * 8 + 255) / 256 * 256;
