@@ -510,13 +510,15 @@ def _table(dev, t):
     return t.data_ptr(), stride[0]
 
 
-def _heads(dev, name, t, n, H, Dh):
-    """Address and token stride of a bf16 tensor [at least n rows, H, Dh], a row's heads contiguous, on device number dev."""
-    bf16 = (_of_tensor or _tensor_methods())[1]
-    shape, stride = t.shape, t.stride()
-    if (t.dtype is not bf16 or t.get_device() != dev or len(shape) != 3 or shape[0] < n or shape[1] != H or shape[2] != Dh
-            or stride[2] != 1 or (stride[1] != Dh and H > 1)):
-        raise ValueError(f"{name} must be a bf16 tensor [{n}, {H}, {Dh}] of contiguous rows on the call's device, " + _got(t))
+def _heads(dev, name, t, rows):
+    """Address and token stride of a bf16 tensor of rows = (n, H, Dh) (or more of them), a row's heads contiguous, on
+    device number dev."""
+    bf16, stride = (_of_tensor or _tensor_methods())[1], t.stride()
+    if t.shape != rows:
+        if t.dim() != 3 or t.shape[0] < rows[0] or t.shape[1:] != rows[1:]:
+            raise ValueError(f"{name} must be a tensor {list(rows)}, " + _got(t))
+    if t.dtype is not bf16 or t.get_device() != dev or stride[2] != 1 or (stride[1] != rows[2] and rows[1] > 1):
+        raise ValueError(f"{name} must be a bf16 tensor {list(rows)} of contiguous rows on the call's device, " + _got(t))
     return t.data_ptr(), stride[0]
 
 
@@ -604,7 +606,7 @@ def wam_rope_qkv_paged(cache: wam_paged_cache, qkv, pos, slots, q_out, pairs, ha
     if qkv.dtype is not bf16 or stride[1] != 1 or width % cache.Dh:
         raise ValueError(f"qkv must be a bf16 tensor of contiguous rows of whole heads of {cache.Dh}, " + _got(qkv))
     pos, slots = _ints(dev, "pos slots", (T * n, T), (pos, slots))
-    q, q_stride = (None, 0) if q_out is None else _heads(dev, "q_out", q_out, T, Hq, cache.Dh)
+    q, q_stride = (None, 0) if q_out is None else _heads(dev, "q_out", q_out, (T, Hq, cache.Dh))
     _cache_on(cache, dev)
     d = wam_rope_paged_desc(T=T, Hq=Hq, n_axes=n, halves=int(halves), theta=theta, qkv_tok_stride=stride[0], q_tok_stride=q_stride)
     d.pairs[:min(n, WAM_ROPE_MAX_AXES)] = pairs[:WAM_ROPE_MAX_AXES]
@@ -621,9 +623,10 @@ def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, w
     """q, o [T, Hq, Dh] bf16 (token strides from the tensors); block_table [R, max_pages], q_start [R + 1],
     kv_len and q_len [R] contiguous int32; max_kv (default: what the table's width can hold) bounds kv_len; ws a uint8
     device tensor of at least wam_attn_paged_workspace_bytes(cache, R, T, Hq, max_kv)."""
-    (T, Hq, _), dev, (R, width), Dh = q.shape, q.get_device(), block_table.shape, cache.Dh
-    qp, q_stride = _heads(dev, "q", q, T, Hq, Dh)
-    op, o_stride = _heads(dev, "o", o, T, Hq, Dh)
+    (T, Hq, _), dev, (R, width) = q.shape, q.get_device(), block_table.shape
+    rows = T, Hq, cache.Dh
+    qp, q_stride = _heads(dev, "q", q, rows)
+    op, o_stride = _heads(dev, "o", o, rows)
     table, stride = _table(dev, block_table)
     if q_len is None:
         q_start, kv_len = _ints(dev, "q_start kv_len", (R + 1, R), (q_start, kv_len))
@@ -645,11 +648,13 @@ def wam_attn_cross(q, k, v, q_start, k_start, o, ws=None, max_k=None, q_len=None
     """q, o [T, Hq, Dh] bf16; k, v [S, Hkv, Dh] bf16 views (token strides from the tensors); q_start [R + 1], q_len
     [R] or None, k_start [R] with k_len [R], or [R + 1] without, all contiguous int32; max_k (default S) bounds k_len; ws a
     uint8 device tensor of at least wam_attn_cross_workspace_bytes(R, T, Hq, Hkv, Dh, max_k)."""
-    (T, Hq, Dh), dev, (S, Hkv, _), R = q.shape, q.get_device(), k.shape, q_start.shape[0] - 1
-    qp, q_stride = _heads(dev, "q", q, T, Hq, Dh)
-    op, o_stride = _heads(dev, "o", o, T, Hq, Dh)
-    kp, kv_stride = _heads(dev, "k", k, S, Hkv, Dh)
-    vp, v_stride = _heads(dev, "v", v, S, Hkv, Dh)
+    rows, dev, (S, Hkv, _), R = q.shape, q.get_device(), k.shape, q_start.shape[0] - 1
+    T, Hq, Dh = rows
+    keys = S, Hkv, Dh
+    qp, q_stride = _heads(dev, "q", q, rows)
+    op, o_stride = _heads(dev, "o", o, rows)
+    kp, kv_stride = _heads(dev, "k", k, keys)
+    vp, v_stride = _heads(dev, "v", v, keys)
     if v_stride != kv_stride:
         raise ValueError("k and v must share the token stride")
     names, sizes, ints = "q_start k_start", (R + 1, R + (k_len is None)), (q_start, k_start)
