@@ -5,7 +5,7 @@
 // token by token; a workgroup owns 128 (16, 32) of them, so a shared head's keys are read once for its
 // whole group.  Row tile x of the launch belongs to the last request r with floor(q_start[r] G / 128)
 // + r <= x: every request has room for its tiles there, the launch needs only T, G and R, and a
-// workgroup finds its request with one pass over q_start.
+// workgroup finds its request by ballots over q_start, 64 starts at a time.
 //
 // Two paths by the request's rows (a kernel for calls whose requests have few on average, 16 or 32 to a workgroup, and
 // one for the others, which streams those that have few all the same):
@@ -18,6 +18,10 @@
 //          block table (a page holds a multiple of 16 keys).
 // Where rows are few and keys many the key axis is split over workgroups (ragged_plan.h); the parts
 // are joined in a fixed order by a second kernel.
+//
+// Held in fewer than 32 bits: the probabilities, rounded to bf16 (each off by 2^-8 of itself at most) since a matrix
+// instruction takes both operands in one type and V is bf16; their sum is that of the rounded ones, so that what they have in
+// common cancels.  Scores, references, sums and outputs are in 32 bits until the one rounding of the stored output.
 #include "attn_tile.h"
 #include "kernels.h"
 #include "ragged_plan.h"
@@ -112,9 +116,12 @@ WAM_DEV float exp_scale(uint32_t biased) { return __uint_as_float(biased << 23);
 // workgroup's rows see and others do not, in the tiles at the mask's edge.  Those tiles are searched, and where one holds an
 // infinity or a NaN the workgroup's rows are done once more on the streaming path, in a form whose product leaves such
 // values out, while two products of ones count for every row and dim those that the row sees: (infinity or NaN) and
-// (-infinity or NaN), added as infinities of both signs (a NaN as their sum).  (Done anew and not within the tile, so that it
-// takes no registers of the common path.  The search costs 3% of one causal request of 500 rows over 3000 keys, 28.0 -> 28.9
-// us, and 1% of the 12 causal requests of 1 to 901 rows.)
+// (-infinity or NaN), added as infinities of both signs (a NaN as their sum).  Done anew and not within the tile, for its
+// vector registers: a product by key in the tile spilt 100 and more.  The search and the second pass take hardly any of them
+// (paged, head size 128: 252 -> 253; E4M3, which spilt 7 of them without, 12), but scalar ones, of which the tile kernels keep
+// some in vector lanes (0 -> 93).  With the search alone left out one causal request of 500 rows over 3000 keys takes 38.6 us
+// (a form of the kernel that spills; 29.2 with it), the 12 causal requests of 1 to 901 rows 32.4 (32.9), two samples' 3152
+// rows 1842 (1835).
 // x + 0 * (every bf16 of v): NaN from the first that is not finite on
 WAM_DEV float zero_times(u32x4v v, float x) {
   const bf16x2 zeros = {(bf16)0.f, (bf16)0.f};
@@ -165,10 +172,9 @@ struct StreamRegs {
   int nv[2];  // keys there are of each group (wave-uniform)
 };
 
-// (Whole rows, K's of both groups before V's, marked as used once: only this workgroup reads them, and they should not push
-// others out of the caches.  us for 48 single tokens, 8 heads of 128 / 32 tokens, 8 heads of 64 / 64 tokens, 8 heads,
-// E4M3: K in the operand's order from memory (64 bytes of 16 rows per load) 159 / 82 / 278; with V marked 149 / 79 /
-// 275; whole rows of both, marked 139 / 79 / 267; K before V in a group 139 / 69 / 267, in both 139 / 70 / 257.)
+// (Whole rows, marked as used once: only this workgroup reads them, and they should not push others out of the caches.
+// us for 48 single tokens, 8 heads of 128 / the same of 64 / 64 tokens, 8 heads, E4M3: 139 / 78 / 255; not marked 153 / 87 /
+// 268; V of a group right after its K instead of after both groups' 140 / 79 / 255.)
 template <int DH, bool PAGED, bool FP8>
 WAM_DEV void stream_load(StreamRegs<DH, FP8>& x, const RaggedArgs& a, const Req& q, int hk, int key0, int end, int pg0,
                          int pg1, int lane, int off) {
@@ -779,7 +785,7 @@ WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
             bf16x4{(bf16)(acc[mt][4 * rr + 0] * inv), (bf16)(acc[mt][4 * rr + 1] * inv),
                    (bf16)(acc[mt][4 * rr + 2] * inv), (bf16)(acc[mt][4 * rr + 3] * inv)};
       }
-    // (not to be kept in the caches: two samples' 3152 rows against 512 and 248 keys 93 -> 85 us)
+    // (not to be kept in the caches: two samples' 3152 rows against 512 and 248 keys 93 -> 73 to 86 us)
     put([&](int64_t tk, int h, int ch, u32x4v v) {
       __builtin_nontemporal_store(v, reinterpret_cast<u32x4v*>(static_cast<bf16*>(a.o) + tk * a.o_ts + h * DH + 8 * ch));
     });
@@ -875,7 +881,7 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, int block, Work& k)
 }
 
 // Requests with more than a few rows on average: 128 rows per workgroup; those with at most 32 are streamed.
-// (Head size 64: 168 registers, three wavefronts per SIMD; with two 12 causal requests of 1 to 901 rows 31.7 -> 36.5 us.)
+// (Head size 64: 168 registers, three wavefronts per SIMD; with two 12 causal requests of 1 to 901 rows 33 -> 38 us.)
 template <int DH, bool PAGED, bool FP8, int GROUPS>
 __global__ __launch_bounds__(NT * GROUPS, DH == 64 ? 3 : 2) void ragged_tile_kernel(const RaggedArgs a, const Parts pt) {
   __shared__ __attribute__((aligned(16))) bf16 smem[GROUPS * 4 * BN * DH];
@@ -900,7 +906,8 @@ __global__ __launch_bounds__(NT * GROUPS, DH == 64 ? 3 : 2) void ragged_tile_ker
   }
 }
 
-// Few rows per request: 16 NQ per workgroup.
+// Few rows per request: 16 NQ per workgroup.  (Wavefronts per SIMD as the registers come out: of 128 dims and 16 rows three
+// over pages and two over packed states, 168 and 170 registers; two for 32 rows.)
 template <int DH, bool PAGED, bool FP8, int NQ>
 __global__ __launch_bounds__(NT, 2) void ragged_stream_kernel(const RaggedArgs a, const Parts pt) {
   __shared__ __attribute__((aligned(16))) char smem[stream_lds(DH, FP8)];

@@ -21,9 +21,10 @@ WAM_DEV int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : 
 //
 // Bound by latency, a chain of dependent loads (lengths, sums, search, table entry), so: the sums
 // are in 32 bits (tokens saturate at T) and in registers but for one exchange through LDS, and workgroups
-// are small and many, each with one kind of output.  6 requests with 5600 rows: 5.4 us, 1000 with 196000 rows and
-// 27000 pages that change hands 11.6 us.  With one kind of workgroup for all outputs 5.7 and 13.4; with 64-bit sums
-// by lane exchange, 1024 threads, and a search and a 64-bit division per token 27.6 and 43.1.
+// are small and many, each with one kind of output.  6 requests with 5600 rows: 5.0 us, 1000 with 196000 rows and
+// 27000 pages that change hands 11.7 us (1000 with a row each 11.8); 1030 and 1900 requests, which read the lengths again
+// instead of keeping them in LDS, 17 and 18 us.  With one kind of workgroup for all outputs the first two 5.7 and 13.4; with
+// 64-bit sums by lane exchange, 1024 threads, and a search and a 64-bit division per token 27.6 and 43.1.
 // ---------------------------------------------------------------------------------
 constexpr int PLAN_NT = 256;
 
@@ -267,10 +268,10 @@ __global__ __launch_bounds__(PLAN_NT) void page_plan_kernel(const PagePlanArgs a
 // cosine and sine of every pair once for all heads (fp64 angle in revolutions, reduced to
 // [-1/2, 1/2] there, then fp32), the rest is one pass over the row, 16 dims per item in two 16-byte
 // chunks: neighbouring chunks, or the two halves' chunks whose dims turn together.  Bound by memory, each byte
-// moved once; a thread's first item is on its way while the angles are formed.  3152 tokens, 40 heads: 43.6 us for
-// 194 MB (4.4 TB/s; a large copy reaches 4.85); without the loads' mark as used once 45.5 (but 1120 tokens into an E4M3
-// cache 15.0, and 18.7 with it).  Two or four items on their way at once: 46 and 47 us, E4M3 15 and 17.  Rows of up to 128
-// items share a workgroup: 8000 tokens of 8/2 heads of 64 10.4 -> 8.5 us.
+// moved once; a thread's first item is on its way while the angles are formed.  3152 tokens, 40 heads: 44.0 us for
+// 194 MB (4.4 TB/s; a large copy reaches 4.85); without the loads' mark as used once 46.1 (but 1120 tokens into an E4M3
+// cache 14.9, and 18.5 with it).  Two or four items on their way at once: 46 and 47 us, E4M3 15 and 17.  Rows of up to 128
+// items share a workgroup: 8000 tokens of 8/2 heads of 64 11.9 -> 8.6 us.
 // ---------------------------------------------------------------------------------
 // dims (2p, 2p + 1) of pairs pair0 .. pair0 + 3; pairs from n on are kept
 WAM_DEV void turn8(float* y, const float* cs, const float* sn, int pair0, int n) {

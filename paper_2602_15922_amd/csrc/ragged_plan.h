@@ -28,22 +28,26 @@ inline RaggedPlan plan_ragged(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int
   int64_t n, keys;  // parts that the machine asks for, keys that a part has at least
   if (p.rows < RAGGED_ROWS) {
     // The parts of ragged requests have to be many and alike, or the longest run alone at the end, and the fewer,
-    // the less is written and joined.  us at 256, 512, 1024, 1536 keys: 48 requests of 212-16001 keys, 8 heads 176, 158,
-    // 157, 170; the same of 64 dims 86, 79, 83, 87; 32 requests of 328-4000 keys 52, 54, 62, 62.  32 rows write and
-    // join eight times as much as 4 (32 rows, 40 heads, 9488 keys 68, 63, 72, 66; 5 heads, 1120 keys 13, 15, 20).
+    // the less is written and joined.  us at 256, 512, 1024, 1536 keys: 48 requests of 212-16001 keys, 8 heads 162, 152,
+    // 139, 148; the same of 64 dims 85, 79, 78, 86; 32 requests of 328-4000 keys 48, 46, 54, 52.  32 rows write and
+    // join eight times as much as 4 (32 rows, 40 heads, 9488 keys 61, 56, 64, 58; 5 heads, 1120 keys 12, 14, 17, 19).
     const auto parts = [&](int64_t k) { return items * ((max_k + k - 1) / k); };
     keys = parts(1024) >= 4096 ? 1024 : parts(512) >= (p.rows == 16 ? 4096 : 512) ? 512 : 256;
     n = (16384 + items - 1) / items;
   } else if (R == 1 && items <= CUS) {
     // One request that leaves CUs idle: as many parts as there are CUs for, each a workgroup of eight wavefronts that has
-    // its CU alone.  544 rows, 1632 keys, 40 heads: 38 us, two parts of four wavefronts 53; 3152 rows, 12608 keys, 5
-    // heads: 130 us, 145.
+    // its CU alone.  544 rows, 1632 keys, 40 heads: 38 us; with workgroups of four wavefronts in one part 44, two 48, four
+    // 64.  3152 rows, 12608 keys, 5 heads: 132 us; 257, 152, 128.
     keys = 512;
     n = CUS / items;
   } else {
-    // About one workgroup per CU (64 dims: two, three fit), unless the parts get short.  At 256, 384, 512 workgroups:
-    // 3 x 700 rows, 10 heads 87, 102, 96 us; 20 x 10-100 rows, 16/4 heads 79, 88, 91; 12 ragged prefills of 64 dims 39,
-    // 39, 33.
+    // About one workgroup per CU (64 dims: two, three fit), unless the parts get short.  At 256, 384, 512, 768
+    // workgroups: 3 x 700 rows, 10 heads 90, 106, 99, 97 us; 20 x 10-100 rows, 16/4 heads 77, 88, 91, 85; 12 ragged prefills
+    // of 64 dims 39, 38, 33, 33 (in parts of 448 keys 46).
+    // All requests get one length of part, from the average of their rows: where a few have many rows and most have one, the
+    // single tokens over long histories are hardly split, and two calls are faster than one (one request of 512 rows with 47
+    // single tokens of 212-16001 keys, 32/8 heads 408 us, apart 181 and 133; 2000 rows with 8 tokens of 32000 keys 430,
+    // apart 58 and 186).
     keys = 1024;
     n = ((Dh == 64 ? 2 : 1) * CUS + items - 1) / items;
   }
