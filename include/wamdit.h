@@ -571,7 +571,8 @@ wam_status wam_page_plan(const wam_page_plan_desc* desc, const int32_t* cache_le
  * needed, as in a cache-update pass); the rotated k and v go to row slots[t] % page_size of page
  * slots[t] / page_size of the cache (FP8 cache: encoded as by wam_rope_qkv_fp8).  A token
  * whose slot lies outside [0, n_pages * page_size) is skipped: nothing of it is written.  (Of two tokens with one
- * slot, either may be what the row holds afterwards, also K of one and V of the other.) */
+ * slot, either may be what the row holds afterwards, also K of one and V of the other.)  q_out may be q's own place
+ * (qkv's address and stride); apart from that neither it nor the cache may overlap qkv, pos, slots or each other. */
 #define WAM_ROPE_MAX_AXES 4
 typedef struct {
   int32_t T, Hq, n_axes;
@@ -591,17 +592,21 @@ wam_status wam_rope_qkv_paged(const wam_rope_paged_desc* desc, const wam_paged_c
  *   chunk = 0   all of them;
  *   chunk = c   j < (floor(p / c) + 1) * c: the chunks up to its own, every chunk c tokens
  *               (Appendix C, Figure 10b; c = 1 is causal attention).
- * A row that sees no key (kv_len = 0, absent pages, p < 0) gives 0.  Query head h reads KV head
- * h / (Hq / Hkv); Hq must be a multiple of Hkv, T * Hq < 2^31.  scale <= 0 selects 1/sqrt(Dh); Dh 64 or 128.
+ * A row that sees no key (kv_len = 0, absent pages, p < 0), or none with a score above -infinity, gives 0.
+ * Query head h reads KV head h / (Hq / Hkv); Hq must be a multiple of Hkv, T * Hq < 2^31.  scale <= 0
+ * selects 1/sqrt(Dh); Dh 64 or 128.
  * q, o: [T] rows of [Hq][Dh] bf16 at their token strides (multiples of 8); o must not overlap q
  * or the cache.  With an FP8 cache K and V are decoded (exactly, to bf16; v_scale is applied in
  * fp32) and q stays bf16.  Rows of the cache that hold no key of a request are not used,
- * whatever they hold, and a NaN or infinity of a key reaches the rows that see it and no others.
+ * whatever they hold, and a NaN or infinity of a key's K or V reaches the rows that see the key and
+ * no others, through its score or its weight (a weight of 0 in 32 bits times an infinity is NaN).
  * max_kv <= 2^30 bounds kv_len (longer ones are cut); it, R, T and the heads choose how the key axis
  * is split, and with that the rounding; a call repeated gives the same bits (no atomics), and a
- * row's do not depend on what the other requests hold.  ws: wam_attn_paged_workspace_bytes(desc, cache) bytes
- * (may be 0: then ws may be NULL), 256-byte aligned; calls that may overlap in time need
- * workspaces of their own. */
+ * row's do not depend on what the other requests hold.  The parts are one length for all requests: give
+ * the longest kv_len where the host knows it, not a capacity, and where histories are long, requests of
+ * many rows and single tokens in calls of their own.
+ * ws: wam_attn_paged_workspace_bytes(desc, cache) bytes (may be 0: then ws may be NULL), 256-byte
+ * aligned; calls that may overlap in time need workspaces of their own. */
 typedef struct {
   int32_t R, T, Hq, max_pages, max_kv, chunk;
   int64_t table_stride;
