@@ -569,7 +569,8 @@ wam_status wam_page_plan(const wam_page_plan_desc* desc, const int32_t* cache_le
  * near one; the rotation is in fp32, rounded once.
  * q_out [T] rows (stride q_tok_stride) of [Hq][Dh] bf16 receives the rotated q (NULL: q is not
  * needed, as in a cache-update pass); the rotated k and v go to row slots[t] % page_size of page
- * slots[t] / page_size of the cache (FP8 cache: encoded as by wam_rope_qkv_fp8).  A token
+ * slots[t] / page_size of the cache (FP8 cache: encoded as by wam_rope_qkv_fp8, for finite k and v:
+ * E4M3 saturates an infinity, and a NaN becomes a finite code).  A token
  * whose slot lies outside [0, n_pages * page_size) is skipped: nothing of it is written.  (Of two tokens with one
  * slot, either may be what the row holds afterwards, also K of one and V of the other.)  q_out may be q's own place
  * (qkv's address and stride); apart from that neither it nor the cache may overlap qkv, pos, slots or each other. */
