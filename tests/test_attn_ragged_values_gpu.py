@@ -73,3 +73,17 @@ def test_cross_values_not_finite_under_a_weight_that_vanishes(q_lens, k_lens, Hq
                 hk = h // (Hq // Hkv)
                 o[rows, h], a[rows, h] = paged_ref.attend(x[rows, h], y[keys, 0, hk], y[keys, 1, hk], np.ones((n, m), bool), Dh ** -0.5)
     check_finite_and_not(run_cross(q, kv, qs, ks), o, a, mine)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh", [([(1, 1), (3, 40)], 4, 2, 128), ([(1, 1500)], 8, 2, 64), ([(150, 400)], 2, 1, 128), ([(150, 2600)], 32, 32, 64)])
+def test_rows_without_a_score_above_minus_infinity(lens, Hq, Hkv, Dh):
+    """Every key of KV head 0 scores -infinity: its rows are 0, as of a row that sees no key; the other heads' are as ever."""
+    b = Batch(lens, Hq, Hkv, Dh, 16, seed=81 + Dh)
+    b.q[..., 5] = 1
+    o, a, mine = b.expected(1)
+    b.k[..., 0, 5] = float("-inf")
+    log(f"paged scores of -infinity {lens} Hq={Hq} Dh={Dh}")
+    got, G = run_paged(b, 1), Hq // Hkv
+    assert np.all(got[mine][:, :G] == 0)
+    o, a, rest = o[:, G:], a[:, G:], got[:, G:]
+    assert np.all((np.abs(rest - o) <= paged_ref.attention_tolerance(a))[mine]) and np.all(got[~mine] == OLD)
