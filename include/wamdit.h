@@ -637,6 +637,139 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
                           const int32_t* k_len, void* o, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------------
+ * Requests that branch: several futures (drafted tokens as a tree, candidate action or video chunks) over one history.
+ *
+ * A turn of a tree of drafted tokens: wam_page_plan and wam_rope_qkv_paged as for any new tokens (a token's rotary position is
+ * its depth's), wam_attn_tree for every layer, wam_verify_tree on the probabilities, wam_cache_compact for every layer, and
+ * the plan of the next turn with the cache_len that the verification wrote, which takes back the pages past it.  Branches that go on as
+ * requests of their own: wam_page_fork and, for every layer, wam_page_copy.  "Ragged rows" and "Device values" as above.
+ *
+ * Shared pages  A forked page is named by several rows of the table.  wam_page_plan gives the surplus pages of a request to the
+ *   stack whoever else names them; where pages are shared, wam_page_collect with the same cache_len comes first, and the plan
+ *   (with collect's held_out and n_free_out) finds no surplus.  A token is written (plan's slots) only to pages
+ *   past a request's history and to its last one, which the fork copied; nothing else may shorten a history below what it shares
+ *   and then write there.
+ * ------------------------------------------------------------------------------ */
+
+/* wam_page_fork — requests that begin as the history of others.
+ *
+ * Fork i makes request dst[i], which holds no page (held = 0), begin as the tokens [f, f + len[i]) of request src[i], f =
+ * first[i] * page_size (first NULL: 0; whole pages at the front may be left out, as by a sliding window).  The pages that
+ * these tokens fill are shared: table[dst][j] = table[src][first + j], j < w = floor(len / page_size).  The last, if it is
+ * filled in part, gets a page of its own, the forks' in their order from the top of the stack: table[dst][w]; copies[i] = (source
+ * page, that page, len % page_size rows) says what wam_page_copy has to copy, (-1, -1, 0) where there is nothing.  With no page
+ * on the stack any more the entry is -1 (an absent page).
+ * A fork with src or dst outside [0, R), a dst that holds pages or that an earlier fork names, first or len negative, or tokens
+ * past the pages that src holds, does nothing.
+ * Written: the table's entries named above; copies [N][3]; and
+ *   held_out [R]    pages that each request holds now;   n_free_out [1]
+ *   status [2]      pages missing; forks that do nothing and values of held and n_free outside their range (cut to it)
+ * free_list [n_pages] and n_free as for wam_page_plan, not written.  No written buffer may overlap any other.  A call repeated
+ * on the same inputs gives the same result.  R, N <= WAM_PLAN_MAX_REQUESTS; R * max_pages < 2^31.  No workspace. */
+typedef struct {
+  int32_t R, N, page_size, n_pages, max_pages;
+  int64_t table_stride;
+} wam_page_fork_desc;
+wam_status wam_page_fork(const wam_page_fork_desc* desc, const int32_t* src, const int32_t* dst, const int32_t* first,
+                         const int32_t* len, const int32_t* held, const int32_t* n_free, int32_t* block_table,
+                         const int32_t* free_list, int32_t* held_out, int32_t* n_free_out, int32_t* copies,
+                         int32_t* status, hipStream_t stream);
+
+/* wam_page_copy — the first copies[i][2] rows of page copies[i][0] (K, V and the exponents of an FP8 cache) to page
+ * copies[i][1], of one layer's cache; copies [N][3] as wam_page_fork writes them.  An entry with a page outside the pool or no rows
+ * does nothing; rows past page_size are cut.  The copies may run in any order: no page may be the target of two entries, nor
+ * the source of one and the target of another (of such pages the rows of any of them, or a mix, are left). */
+wam_status wam_page_copy(const wam_paged_cache* cache, int32_t N, const int32_t* copies, hipStream_t stream);
+
+/* wam_page_collect — the stack of free pages from what the requests still name, shared or not.
+ *
+ * Request r keeps the first cache_len[r] tokens of its history (0: it has ended), and of the held[r] pages that it holds the
+ * first min(held, ceil(cache_len / page_size)) = held_out[r].  Every page of the pool that no request keeps is free:
+ * free_list [0, n_free_out) are these pages, ascending (entries past them are left as they were).
+ *   status [2]   kept entries of the table that name no page; invalid inputs (cache_len negative, held outside
+ *                [0, max_pages]: cut to its range)
+ * No page is counted by its holders, so none can be lost or freed twice; pages that must stay without a request (a prompt
+ * that many begin with) are a row of the table of their own.  No written buffer may overlap any other.
+ * R <= WAM_PLAN_MAX_REQUESTS, R * max_pages < 2^31, n_pages <= WAM_COLLECT_MAX_PAGES.  No workspace. */
+#define WAM_COLLECT_MAX_PAGES (1 << 20)
+typedef struct {
+  int32_t R, page_size, n_pages, max_pages;
+  int64_t table_stride;
+} wam_page_collect_desc;
+wam_status wam_page_collect(const wam_page_collect_desc* desc, const int32_t* cache_len, const int32_t* held,
+                            const int32_t* block_table, int32_t* free_list, int32_t* held_out, int32_t* n_free_out,
+                            int32_t* status, hipStream_t stream);
+
+/* wam_cache_compact — the rows of the new tokens that a request keeps, moved together (one layer's cache).
+ *
+ * Request r's n = q_len[r] new tokens are the last of its kv_len[r]; it keeps m = n_keep[r] of them, numbers keep[q_start[r] + i]
+ * in [0, n), i < m, ascending.  Row kv_len - n + keep[i] of its K, V and exponents goes to kv_len - n + i, all of them as they
+ * were before the call; the rows past kv_len - n + m keep what they hold.  (The path of wam_verify_tree is such a list.)
+ * A number outside [0, n) and rows of absent pages are left out.  Numbers that do not ascend leave the rows that they name with values of
+ * some of them (the same at every call).  The rows' pages may belong to no other request. */
+typedef struct {
+  int32_t R, T, max_pages;
+  int64_t table_stride;
+} wam_cache_compact_desc;
+wam_status wam_cache_compact(const wam_cache_compact_desc* desc, const wam_paged_cache* cache, const int32_t* block_table,
+                             const int32_t* q_start, const int32_t* q_len, const int32_t* kv_len, const int32_t* keep,
+                             const int32_t* n_keep, hipStream_t stream);
+
+/* wam_attn_tree — wam_attn_paged in which the new tokens see each other by a mask.
+ *
+ * Row i of request r (n = q_len[r] rows, the last of its kv_len[r] tokens) sees the history, keys j < kv_len - n, and new token
+ * j (key kv_len - n + j) where bit j % 32 of word j / 32 of its mask row is set: mask [T] rows of mask_words uint32
+ * (4-byte aligned), mask_stride words apart.  A row sees itself only by its own bit.  Bits of tokens that the request does
+ * not have count for nothing, tokens past the mask's 32 * mask_words are seen by nobody.  Trees: the bits of a node's ancestors and its own
+ * (wam_tree_mask); separate futures: the bits of a row's own branch; any other set will do.
+ * All else as for wam_attn_paged: types, heads, scale, absent pages, rows that see no key, values that are not finite, max_kv,
+ * determinism, workspace.  o must not overlap the mask. */
+typedef struct {
+  int32_t R, T, Hq, max_pages, max_kv, mask_words;
+  int64_t table_stride;
+  int64_t q_tok_stride, o_tok_stride, mask_stride;
+  float scale;
+} wam_attn_tree_desc;
+size_t wam_attn_tree_workspace_bytes(const wam_attn_tree_desc* desc, const wam_paged_cache* cache);
+wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* cache, const void* q,
+                         const int32_t* block_table, const int32_t* q_start, const int32_t* q_len,
+                         const int32_t* kv_len, const uint32_t* mask, void* o, void* ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* wam_verify_tree — which drafted tokens of a tree are kept, and the token after them, so that what comes out is distributed as
+ * the target's own samples.
+ *
+ * The nodes of request r are its rows; node 0, the root, is the last token that is already settled.  Node i > 0 stands for the
+ * drafted tokens[q_start + i], a child of node parent[q_start + i], which must lie before it.  p [T] rows of V fp32: the target's
+ * probabilities of the token after each node; q likewise the draft's, from which a node's children were drawn
+ * independently (drawn = 1), or NULL where they were chosen and not drawn (drawn = 0, say a node's likeliest).
+ * From the root on, the children of the present node are tried in order of their numbers: x is taken if
+ *   u[x] s Q(x) < R(x),
+ * where R = P and s = 1 at first, and each rejection replaces R by max(R - s Q, 0) and s by its sum (drawn = 0: Q is a one at x,
+ * so R loses the rejected token).  When no child is left, next_token is drawn from R: the first v with R_0 + .. + R_v >
+ * u_next[r] * (the sum of R) (the last with R_v > 0 if rounding leaves none); from P where the sum of R is 0, -1 where that is 0 too.  With
+ * one-hot rows this is greedy verification.
+ * u [T], u_next [R] in [0, 1) are the caller's random numbers.  Sums are in fp64.  Entries of p that are negative or NaN count as 0.  A
+ * node whose parent does not lie before it or whose token is outside [0, V) is never taken; nor is one past the
+ * first WAM_TREE_MAX_NODES of a request.
+ * Written: path [T]: from entry q_start[r] on the n_path[r] nodes taken, the root first (entries past them are left as they
+ *   were): the list that wam_cache_compact takes; next_token [R]; and cache_len [R] = kv_len - q_len + n_path (both or
+ *   neither given).  A request without rows: n_path 0, next_token -1.
+ * V <= WAM_VERIFY_MAX_VOCAB.  Rows of p and q may lie at any stride >= V and any 4-byte address.  No written buffer may overlap
+ * any other.  ws: wam_verify_tree_workspace_bytes(desc), 256-byte aligned, not shared by calls that may overlap in time. */
+#define WAM_TREE_MAX_NODES 1024
+#define WAM_VERIFY_MAX_VOCAB (1 << 20)
+typedef struct {
+  int32_t R, T, V, drawn;
+  int64_t p_stride, q_stride;
+} wam_verify_tree_desc;
+size_t wam_verify_tree_workspace_bytes(const wam_verify_tree_desc* desc);
+wam_status wam_verify_tree(const wam_verify_tree_desc* desc, const float* p, const float* q, const int32_t* tokens,
+                           const int32_t* parent, const float* u, const float* u_next, const int32_t* q_start,
+                           const int32_t* q_len, const int32_t* kv_len, int32_t* path, int32_t* n_path,
+                           int32_t* next_token, int32_t* cache_len, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------------
  * Pieces of the step, exported for testing each kernel on its own.
  * ------------------------------------------------------------------------------ */
 
@@ -815,6 +948,10 @@ wam_status wam_chunk_positions(int32_t c, int32_t F, int32_t Hg, int32_t Wg, int
  * cos_out, sin_out HOST [L][Dh/2]. */
 wam_status wam_rope_tables(const int32_t* pos, int32_t L, int32_t Dh, double theta,
                            float* cos_out, float* sin_out);
+
+/* Rows of wam_attn_tree's mask for a tree: HOST parent [n] (-1: a root, else a node before it), HOST mask [n][words], the bits
+ * of each node's ancestors and its own; n <= 32 * words. */
+wam_status wam_tree_mask(const int32_t* parent, int32_t n, int32_t words, uint32_t* mask);
 
 #ifdef __cplusplus
 }

@@ -38,6 +38,8 @@ EXPORTED = (
     "wam_cosine_similarity_noalloc", "wam_adaln_ln_mod_fp8", "wam_gemm_fp8_mx",
     "wam_attn_blockcausal_mx", "wam_attn_blockcausal_fp8_mx", "wam_page_plan", "wam_rope_qkv_paged",
     "wam_attn_paged_workspace_bytes", "wam_attn_paged", "wam_attn_cross_workspace_bytes", "wam_attn_cross",
+    "wam_page_fork", "wam_page_copy", "wam_page_collect", "wam_cache_compact", "wam_attn_tree_workspace_bytes",
+    "wam_attn_tree", "wam_verify_tree_workspace_bytes", "wam_verify_tree", "wam_tree_mask",
 )
 
 _vp, _fp, _i32, _i64, _sz = C.c_void_p, C.POINTER(C.c_float), C.c_int32, C.c_int64, C.c_size_t
@@ -159,6 +161,30 @@ class wam_attn_cross_desc(C.Structure):
                [("q_tok_stride", _i64), ("kv_tok_stride", _i64), ("o_tok_stride", _i64), ("scale", C.c_float)]
 
 
+class wam_page_fork_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "N", "page_size", "n_pages", "max_pages")] + [("table_stride", _i64)]
+
+
+WAM_COLLECT_MAX_PAGES, WAM_TREE_MAX_NODES, WAM_VERIFY_MAX_VOCAB = 1 << 20, 1024, 1 << 20
+
+
+class wam_page_collect_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "page_size", "n_pages", "max_pages")] + [("table_stride", _i64)]
+
+
+class wam_cache_compact_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "max_pages")] + [("table_stride", _i64)]
+
+
+class wam_attn_tree_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "Hq", "max_pages", "max_kv", "mask_words")] + \
+               [(n, _i64) for n in ("table_stride", "q_tok_stride", "o_tok_stride", "mask_stride")] + [("scale", C.c_float)]
+
+
+class wam_verify_tree_desc(C.Structure):
+    _fields_ = [(n, _i32) for n in ("R", "T", "V", "drawn")] + [("p_stride", _i64), ("q_stride", _i64)]
+
+
 _lib = None
 
 
@@ -175,7 +201,7 @@ def lib():
                      "wam_cosine_workspace_bytes", "wam_denoise_workspace_bytes",
                      "wam_time_embed_workspace_bytes", "wam_text_proj_workspace_bytes",
                      "wam_embed_workspace_bytes", "wam_head_workspace_bytes", "wam_attn_paged_workspace_bytes",
-                     "wam_attn_cross_workspace_bytes"):
+                     "wam_attn_cross_workspace_bytes", "wam_attn_tree_workspace_bytes", "wam_verify_tree_workspace_bytes"):
             getattr(L, name).restype = _sz
         L.wam_block_workspace_bytes.argtypes = [C.POINTER(wam_dims), _i32, _i32, _i32]
         L.wam_step_workspace_bytes.argtypes = [C.POINTER(wam_model), C.POINTER(wam_step_io)]
@@ -233,6 +259,15 @@ def lib():
         L.wam_attn_paged.argtypes = [C.POINTER(wam_attn_paged_desc), C.POINTER(wam_paged_cache)] + [_vp] * 7 + [_sz, _vp]
         L.wam_attn_cross_workspace_bytes.argtypes = [C.POINTER(wam_attn_cross_desc)]
         L.wam_attn_cross.argtypes = [C.POINTER(wam_attn_cross_desc)] + [_vp] * 9 + [_sz, _vp]
+        L.wam_page_fork.argtypes = [C.POINTER(wam_page_fork_desc)] + [_vp] * 13
+        L.wam_page_copy.argtypes = [C.POINTER(wam_paged_cache), _i32, _vp, _vp]
+        L.wam_page_collect.argtypes = [C.POINTER(wam_page_collect_desc)] + [_vp] * 8
+        L.wam_cache_compact.argtypes = [C.POINTER(wam_cache_compact_desc), C.POINTER(wam_paged_cache)] + [_vp] * 7
+        L.wam_attn_tree_workspace_bytes.argtypes = [C.POINTER(wam_attn_tree_desc), C.POINTER(wam_paged_cache)]
+        L.wam_attn_tree.argtypes = [C.POINTER(wam_attn_tree_desc), C.POINTER(wam_paged_cache)] + [_vp] * 8 + [_sz, _vp]
+        L.wam_verify_tree_workspace_bytes.argtypes = [C.POINTER(wam_verify_tree_desc)]
+        L.wam_verify_tree.argtypes = [C.POINTER(wam_verify_tree_desc)] + [_vp] * 14 + [_sz, _vp]
+        L.wam_tree_mask.argtypes = [C.POINTER(_i32), _i32, _i32, C.POINTER(C.c_uint32)]
         for name in EXPORTED[2:]:
             if not name.endswith("_bytes"):
                 getattr(L, name).restype = C.c_int
@@ -637,6 +672,131 @@ def wam_attn_paged(cache: wam_paged_cache, q, block_table, q_start, kv_len, o, w
                             stride, q_stride, o_stride, scale)
     _check(lib().wam_attn_paged(C.byref(d), C.byref(cache), qp, table, q_start, q_len, kv_len, op, *_workspace(dev, ws),
                                 _stream_on(stream, dev)))
+
+
+def wam_page_fork(src, dst, first, length, held, n_free, block_table, free_list, held_out, n_free_out, copies, status,
+                  page_size: int, stream=None):
+    """All contiguous int32 device tensors: src, dst, length and first (or None) [N]; held, held_out [R]; n_free, n_free_out
+    [1]; block_table [R, max_pages] (its rows may lie apart); free_list [n_pages]; copies [N, 3]; status [2].  Nothing that
+    is written may overlap anything else."""
+    (R, width), N, dev = block_table.shape, src.shape[0], block_table.get_device()
+    table, stride = _table(dev, block_table)
+    names, sizes = "src dst length held n_free free_list held_out n_free_out copies status", (N, N, N, R, 1, 0, R, 1, 3 * N, 2)
+    ints = src, dst, length, held, n_free, free_list, held_out, n_free_out, copies, status
+    if first is not None:
+        names, sizes, ints = names + " first", sizes + (N,), ints + (first,)
+    src, dst, length, held, n_free, stack, held_out, n_free_out, copies, status, *skip = _ints(dev, names, sizes, ints)
+    d = wam_page_fork_desc(R, N, page_size, free_list.shape[0], width, stride)
+    _check(lib().wam_page_fork(C.byref(d), src, dst, skip[0] if skip else None, length, held, n_free, table, stack, held_out,
+                               n_free_out, copies, status, _stream_on(stream, dev)))
+
+
+def wam_page_copy(cache: wam_paged_cache, copies, stream=None):
+    """copies [N, 3] contiguous int32: source page, target page, rows."""
+    if copies.dim() != 2 or copies.shape[1] != 3:
+        raise ValueError("copies must have three columns, " + _got(copies))
+    N, dev = copies.shape[0], copies.get_device()
+    (ptr,) = _ints(dev, "copies", (3 * N,), (copies,))
+    _cache_on(cache, dev)
+    _check(lib().wam_page_copy(C.byref(cache), N, ptr, _stream_on(stream, dev)))
+
+
+def wam_page_collect(cache_len, held, block_table, free_list, held_out, n_free_out, status, page_size: int, stream=None):
+    """All contiguous int32 device tensors: cache_len, held, held_out [R]; block_table [R, max_pages] (its rows may lie apart);
+    free_list [n_pages]; n_free_out [1]; status [2].  Nothing that is written may overlap anything else."""
+    (R, width), dev = block_table.shape, block_table.get_device()
+    table, stride = _table(dev, block_table)
+    n_pages = free_list.shape[0]
+    cache_len, held, free_list, held_out, n_free_out, status = _ints(
+        dev, "cache_len held free_list held_out n_free_out status", (R, R, n_pages, R, 1, 2),
+        (cache_len, held, free_list, held_out, n_free_out, status))
+    d = wam_page_collect_desc(R, page_size, n_pages, width, stride)
+    _check(lib().wam_page_collect(C.byref(d), cache_len, held, table, free_list, held_out, n_free_out, status,
+                                  _stream_on(stream, dev)))
+
+
+def wam_cache_compact(cache: wam_paged_cache, block_table, q_start, kv_len, keep, n_keep, q_len=None, stream=None):
+    """block_table [R, max_pages], q_start [R + 1], kv_len, n_keep and q_len (or None) [R], keep [T], all contiguous int32
+    (the table's rows may lie apart)."""
+    (R, width), T, dev = block_table.shape, keep.shape[0], block_table.get_device()
+    table, stride = _table(dev, block_table)
+    names, sizes, ints = "q_start kv_len keep n_keep", (R + 1, R, T, R), (q_start, kv_len, keep, n_keep)
+    if q_len is not None:
+        names, sizes, ints = names + " q_len", sizes + (R,), ints + (q_len,)
+    q_start, kv_len, keep, n_keep, *lens = _ints(dev, names, sizes, ints)
+    _cache_on(cache, dev)
+    d = wam_cache_compact_desc(R, T, width, stride)
+    _check(lib().wam_cache_compact(C.byref(d), C.byref(cache), table, q_start, lens[0] if lens else None, kv_len, keep, n_keep,
+                                   _stream_on(stream, dev)))
+
+
+def wam_attn_tree_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: int, max_kv: int) -> int:
+    d = wam_attn_tree_desc(R=R, T=T, Hq=Hq, max_kv=max_kv)
+    return lib().wam_attn_tree_workspace_bytes(C.byref(d), C.byref(cache))
+
+
+def wam_attn_tree(cache: wam_paged_cache, q, block_table, q_start, kv_len, mask, o, ws=None, max_kv=None, q_len=None,
+                  scale=0.0, stream=None):
+    """As wam_attn_paged, with mask [T, words] int32 (or more rows; a row's words contiguous): bit j % 32 of word j / 32 of a
+    row says whether it sees its request's new token j.  ws: wam_attn_tree_workspace_bytes(cache, R, T, Hq, max_kv)."""
+    (T, Hq, _), dev, (R, width) = q.shape, q.get_device(), block_table.shape
+    rows = T, Hq, cache.Dh
+    qp, q_stride = _heads(dev, "q", q, rows)
+    op, o_stride = _heads(dev, "o", o, rows)
+    table, stride = _table(dev, block_table)
+    bits, words = mask.stride(), mask.shape[-1]
+    if mask.dtype is not (_of_tensor or _tensor_methods())[0] or len(bits) != 2 or mask.shape[0] < T or \
+            (bits[1] != 1 and words > 1) or mask.get_device() != dev:
+        raise ValueError(f"mask must be an int32 tensor [{T}, words] of contiguous rows on the call's device, " + _got(mask))
+    if q_len is None:
+        q_start, kv_len = _ints(dev, "q_start kv_len", (R + 1, R), (q_start, kv_len))
+    else:
+        q_start, kv_len, q_len = _ints(dev, "q_start kv_len q_len", (R + 1, R, R), (q_start, kv_len, q_len))
+    _cache_on(cache, dev)
+    d = wam_attn_tree_desc(R, T, Hq, width, min(width * cache.page_size, 1 << 30) if max_kv is None else max_kv, words,
+                           stride, q_stride, o_stride, max(bits[0], words), scale)
+    _check(lib().wam_attn_tree(C.byref(d), C.byref(cache), qp, table, q_start, q_len, kv_len, mask.data_ptr(), op,
+                               *_workspace(dev, ws), _stream_on(stream, dev)))
+
+
+def wam_verify_tree_workspace_bytes(R: int, T: int, V: int, drawn: bool) -> int:
+    d = wam_verify_tree_desc(R, T, V, int(drawn), V, V)
+    return lib().wam_verify_tree_workspace_bytes(C.byref(d))
+
+
+def wam_verify_tree(p, q, tokens, parent, u, u_next, q_start, path, n_path, next_token, ws, q_len=None, kv_len=None,
+                    cache_len=None, stream=None):
+    """p [T, V] fp32 (rows at any stride); q likewise where the drafts were drawn, else None; u [T], u_next [R] contiguous
+    fp32; tokens, parent, path [T], q_start [R + 1], n_path, next_token, q_len, kv_len and cache_len [R] contiguous int32 (the
+    last three may be None); ws of wam_verify_tree_workspace_bytes(R, T, V, drawn)."""
+    import torch
+    (T, V), R, dev, f32 = p.shape, u_next.shape[0], p.get_device(), torch.float32
+    for name, t, shape in (("p", p, (T, V)), ("q", q, (T, V)), ("u", u, (T,)), ("u_next", u_next, (R,))):
+        if t is not None and (t.dtype is not f32 or t.get_device() != dev or t.shape != shape or
+                              (t.stride(-1) != 1 and t.shape[-1] > 1)):
+            raise ValueError(f"{name} must be an fp32 tensor {list(shape)} of contiguous rows on the call's device, " + _got(t))
+    names, sizes = "tokens parent q_start path n_path next_token", (T, T, R + 1, T, R, R)
+    ints, given = (tokens, parent, q_start, path, n_path, next_token), []
+    for name, t in (("q_len", q_len), ("kv_len", kv_len), ("cache_len", cache_len)):
+        if t is not None:
+            names, sizes, ints = f"{names} {name}", sizes + (R,), ints + (t,)
+            given.append(name)
+    tokens, parent, q_start, path, n_path, next_token, *lens = _ints(dev, names, sizes, ints)
+    lens = dict(zip(given, lens))
+    d = wam_verify_tree_desc(R, T, V, int(q is not None), max(p.stride(0), V), V if q is None else max(q.stride(0), V))
+    _check(lib().wam_verify_tree(C.byref(d), p.data_ptr(), _p(q), tokens, parent, u.data_ptr(), u_next.data_ptr(), q_start,
+                                 lens.get("q_len"), lens.get("kv_len"), path, n_path, next_token, lens.get("cache_len"),
+                                 *_workspace(dev, ws), _stream_on(stream, dev)))
+
+
+def wam_tree_mask(parent, words=None):
+    """[n, words] int32 rows of wam_attn_tree's mask (host tensor) for a tree: parent [n], -1 for a root, else a node before."""
+    import torch
+    n = len(parent)
+    words = -(-n // 32) if words is None else words
+    mask = torch.zeros(n, words, dtype=torch.int32)
+    _check(lib().wam_tree_mask((_i32 * n)(*parent), n, words, C.cast(mask.data_ptr(), C.POINTER(C.c_uint32))))
+    return mask
 
 
 def wam_attn_cross_workspace_bytes(R: int, T: int, Hq: int, Hkv: int, Dh: int, max_k: int) -> int:

@@ -1,5 +1,5 @@
 // C ABI of the paged KV cache: argument checks and launches of the page plan, the rotary
-// append, and the ragged attentions.
+// append, the ragged attentions, and the operators of requests that branch.
 #include <cmath>
 #include <limits>
 
@@ -105,10 +105,78 @@ bool overlap(const Ints& a, const Ints& b) {
   const int64_t r = d < 0 ? 0 : a.rows == 1 ? d >= a.n : d / a.stride + (d % a.stride >= a.n);
   return r < a.rows && r * a.stride < d + b.n;
 }
+// a table of R rows, and R and the pool's sizes as the page plan takes them
+wam_status check_table(int32_t R, int32_t max_pages, int64_t table_stride, const void* table) {
+  CHECK(R >= 0 && max_pages >= 0, WAM_EINVAL, "negative size (R=%d max_pages=%d)", R, max_pages);
+  CHECK((int64_t)R * max_pages <= INT32_MAX, WAM_EUNSUPPORTED, "R * max_pages must stay below 2^31");
+  CHECK(table_stride >= max_pages && table_stride <= INT64_MAX / 8 / ((int64_t)R + 1), WAM_EINVAL,
+        "table_stride=%lld must be >= max_pages=%d", (long long)table_stride, max_pages);
+  if (R > 0 && max_pages > 0) TRY(need_ints(table, "block_table"));
+  return WAM_OK;
+}
+template <size_t N>
+wam_status check_apart(const Ints (&all)[N]) {
+  for (const Ints& x : all)
+    for (const Ints& y : all) {
+      if (&x == &y || !x.written || (y.written && &y < &x)) continue;
+      // (the one of several rows goes first)
+      CHECK(!(y.rows > 1 ? overlap(y, x) : overlap(x, y)), WAM_EINVAL, "%s and %s overlap", x.name, y.name);
+    }
+  return WAM_OK;
+}
 wam_status check_ws(const void* ws, size_t have, size_t need) {
   CHECK(need == 0 || (ws && (reinterpret_cast<uintptr_t>(ws) & 255) == 0 && have >= need), WAM_EWORKSPACE,
         "workspace of %zu bytes (256-byte aligned) needed, got %zu", need, ws ? have : (size_t)0);
   return WAM_OK;
+}
+
+// attention over pages; a holds what says which keys a row sees
+wam_status run_paged(const wam_attn_paged_desc& d, const wam_paged_cache& c, const void* q, const int32_t* block_table,
+                     const int32_t* q_start, const int32_t* q_len, const int32_t* kv_len, void* o, void* ws, size_t ws_bytes,
+                     RaggedArgs& a, hipError_t (*launch)(const RaggedArgs&, const RaggedPlan&, void*, hipStream_t),
+                     hipStream_t stream) {
+  TRY(check_cache(c));
+  TRY(check_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv));
+  CHECK(d.chunk >= 0, WAM_EINVAL, "chunk=%d is negative", d.chunk);
+  TRY(check_scale(d.scale, c.Dh));
+  CHECK(d.max_pages >= 0 && d.table_stride >= d.max_pages && d.table_stride <= INT64_MAX / 8 / (d.R + 1), WAM_EINVAL,
+        "table_stride=%lld must be >= max_pages=%d >= 0", (long long)d.table_stride, d.max_pages);
+  if (d.R == 0 || d.T == 0) return WAM_OK;
+  TRY(check_rows(q, o, d.q_tok_stride, d.o_tok_stride, (int64_t)d.Hq * c.Dh));
+  TRY(need_ints(q_start, "q_start"));
+  TRY(opt_ints(q_len, "q_len"));
+  TRY(need_ints(kv_len, "kv_len"));
+  if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
+  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
+  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
+  TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, c.Hkv) * 256 * p.groups));
+  a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
+  // (a table without columns is never read: no key is below max_k = 0; its address only says "paged")
+  a.table = block_table ? block_table : q_start;
+  a.q_start = q_start; a.q_len = q_len; a.k_len = kv_len;
+  a.table_stride = d.table_stride; a.q_ts = d.q_tok_stride; a.o_ts = d.o_tok_stride;
+  a.page_stride = c.page_stride; a.tok_stride = c.tok_stride; a.head_stride = c.head_stride;
+  a.R = d.R; a.T = d.T; a.Hq = d.Hq; a.Hkv = c.Hkv; a.Dh = c.Dh; a.n_pages = c.n_pages;
+  a.group = fast_div((uint32_t)(d.Hq / c.Hkv));
+  const int64_t width = (int64_t)d.max_pages * c.page_size;
+  a.max_k = (int32_t)(width < d.max_kv ? width : d.max_kv);
+  a.ps = fast_div((uint32_t)c.page_size);
+  a.c = exp2_scale(d.scale, c.Dh);
+  a.v_scale = c.v_scale;
+  HIPCHECK(launch(a, p, ws, stream));
+  return WAM_OK;
+}
+
+wam_status check_verify(const wam_verify_tree_desc& d) {
+  CHECK(d.R >= 0 && d.T >= 0, WAM_EINVAL, "negative size (R=%d T=%d)", d.R, d.T);
+  CHECK(d.V >= 1, WAM_EINVAL, "V=%d must be positive", d.V);
+  CHECK(d.V <= WAM_VERIFY_MAX_VOCAB, WAM_EUNSUPPORTED, "V=%d exceeds %d", d.V, WAM_VERIFY_MAX_VOCAB);
+  CHECK(d.drawn == 0 || d.drawn == 1, WAM_EINVAL, "drawn=%d must be 0 or 1", d.drawn);
+  CHECK(d.p_stride >= d.V && (!d.drawn || d.q_stride >= d.V), WAM_EINVAL, "the strides of p and q must be >= V=%d", d.V);
+  CHECK(d.p_stride <= INT64_MAX / 8 / ((int64_t)d.T + 1) && (!d.drawn || d.q_stride <= INT64_MAX / 8 / ((int64_t)d.T + 1)),
+        WAM_EINVAL, "a stride of p or q overflows");
+  return check_launch((int64_t)d.R * verify_slices(d) * 256 > (int64_t)d.R * 1024 ? (int64_t)d.R * verify_slices(d) * 256
+                                                                                 : (int64_t)d.R * 1024);
 }
 
 }  // namespace
@@ -231,40 +299,9 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
                           const int32_t* block_table, const int32_t* q_start, const int32_t* q_len,
                           const int32_t* kv_len, void* o, void* ws, size_t ws_bytes, hipStream_t stream) {
   CHECK(desc && cache, WAM_EINVAL, "desc or cache is NULL");
-  const wam_attn_paged_desc& d = *desc;
-  const wam_paged_cache& c = *cache;
-  TRY(check_cache(c));
-  TRY(check_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv));
-  CHECK(d.chunk >= 0, WAM_EINVAL, "chunk=%d is negative", d.chunk);
-  TRY(check_scale(d.scale, c.Dh));
-  CHECK(d.max_pages >= 0 && d.table_stride >= d.max_pages && d.table_stride <= INT64_MAX / 8 / (d.R + 1), WAM_EINVAL,
-        "table_stride=%lld must be >= max_pages=%d >= 0", (long long)d.table_stride, d.max_pages);
-  if (d.R == 0 || d.T == 0) return WAM_OK;
-  TRY(check_rows(q, o, d.q_tok_stride, d.o_tok_stride, (int64_t)d.Hq * c.Dh));
-  TRY(need_ints(q_start, "q_start"));
-  TRY(opt_ints(q_len, "q_len"));
-  TRY(need_ints(kv_len, "kv_len"));
-  if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
-  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
-  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
-  TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, c.Hkv) * 256 * p.groups));
   RaggedArgs a{};
-  a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
-  // (a table without columns is never read: no key is below max_k = 0; its address only says "paged")
-  a.table = block_table ? block_table : q_start;
-  a.q_start = q_start; a.q_len = q_len; a.k_len = kv_len;
-  a.table_stride = d.table_stride; a.q_ts = d.q_tok_stride; a.o_ts = d.o_tok_stride;
-  a.page_stride = c.page_stride; a.tok_stride = c.tok_stride; a.head_stride = c.head_stride;
-  a.R = d.R; a.T = d.T; a.Hq = d.Hq; a.Hkv = c.Hkv; a.Dh = c.Dh; a.n_pages = c.n_pages;
-  a.group = fast_div((uint32_t)(d.Hq / c.Hkv));
-  if (d.chunk > 0) a.chunk = fast_div((uint32_t)d.chunk);
-  const int64_t width = (int64_t)d.max_pages * c.page_size;
-  a.max_k = (int32_t)(width < d.max_kv ? width : d.max_kv);
-  a.ps = fast_div((uint32_t)c.page_size);
-  a.c = exp2_scale(d.scale, c.Dh);
-  a.v_scale = c.v_scale;
-  HIPCHECK(launch_attn_ragged(a, p, ws, stream));
-  return WAM_OK;
+  if (desc->chunk > 0) a.chunk = fast_div((uint32_t)desc->chunk);
+  return run_paged(*desc, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, launch_attn_ragged, stream);
 }
 
 size_t wam_attn_cross_workspace_bytes(const wam_attn_cross_desc* desc) {
@@ -306,6 +343,226 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
   a.group = fast_div((uint32_t)(d.Hq / d.Hkv));
   a.c = exp2_scale(d.scale, d.Dh);
   HIPCHECK(launch_attn_ragged(a, p, ws, stream));
+  return WAM_OK;
+}
+
+wam_status wam_page_fork(const wam_page_fork_desc* desc, const int32_t* src, const int32_t* dst, const int32_t* first,
+                         const int32_t* len, const int32_t* held, const int32_t* n_free, int32_t* block_table,
+                         const int32_t* free_list, int32_t* held_out, int32_t* n_free_out, int32_t* copies,
+                         int32_t* status, hipStream_t stream) {
+  CHECK(desc, WAM_EINVAL, "desc is NULL");
+  const wam_page_fork_desc& d = *desc;
+  CHECK(d.N >= 0, WAM_EINVAL, "N=%d is negative", d.N);
+  CHECK(d.R <= WAM_PLAN_MAX_REQUESTS && d.N <= WAM_PLAN_MAX_REQUESTS, WAM_EUNSUPPORTED, "R=%d or N=%d exceeds %d", d.R, d.N,
+        WAM_PLAN_MAX_REQUESTS);
+  TRY(check_page_size(d.page_size, d.n_pages));
+  TRY(check_table(d.R, d.max_pages, d.table_stride, block_table));
+  if (d.N > 0) {
+    TRY(need_ints(src, "src"));
+    TRY(need_ints(dst, "dst"));
+    TRY(opt_ints(first, "first"));
+    TRY(need_ints(len, "len"));
+    TRY(need_ints(copies, "copies"));
+  }
+  if (d.R > 0) {
+    TRY(need_ints(held, "held"));
+    TRY(need_ints(held_out, "held_out"));
+  }
+  if (d.n_pages > 0) TRY(need_ints(free_list, "free_list"));
+  TRY(need_ints(n_free, "n_free"));
+  TRY(need_ints(n_free_out, "n_free_out"));
+  TRY(need_ints(status, "status"));
+  const Ints all[] = {{"block_table", block_table, d.max_pages, d.R, d.table_stride, true},
+                      {"held_out", held_out, d.R, 1, 0, true},
+                      {"n_free_out", n_free_out, 1, 1, 0, true},
+                      {"copies", copies, 3 * (int64_t)d.N, 1, 0, true},
+                      {"status", status, 2, 1, 0, true},
+                      {"src", src, d.N, 1, 0, false},
+                      {"dst", dst, d.N, 1, 0, false},
+                      {"first", first, d.N, 1, 0, false},
+                      {"len", len, d.N, 1, 0, false},
+                      {"held", held, d.R, 1, 0, false},
+                      {"n_free", n_free, 1, 1, 0, false},
+                      {"free_list", free_list, d.n_pages, 1, 0, false}};
+  TRY(check_apart(all));
+  PageForkArgs a{};
+  a.d = d;
+  a.ps = fast_div((uint32_t)d.page_size);
+  a.src = src; a.dst = dst; a.first = first; a.len = len; a.held = held; a.n_free = n_free; a.free_list = free_list;
+  a.table = block_table; a.held_out = held_out; a.n_free_out = n_free_out; a.copies = copies; a.status = status;
+  HIPCHECK(launch_page_fork(a, stream));
+  return WAM_OK;
+}
+
+wam_status wam_page_copy(const wam_paged_cache* cache, int32_t N, const int32_t* copies, hipStream_t stream) {
+  CHECK(cache, WAM_EINVAL, "cache is NULL");
+  TRY(check_cache(*cache));
+  CHECK(N >= 0, WAM_EINVAL, "N=%d is negative", N);
+  if (N == 0 || cache->n_pages == 0) return WAM_OK;
+  TRY(need_ints(copies, "copies"));
+  const int64_t blocks = page_copy_blocks(*cache);
+  TRY(check_launch(N * blocks * 256));
+  PageCopyArgs a{};
+  a.c = *cache;
+  a.by_blocks = fast_div((uint32_t)blocks);
+  a.by_row = fast_div((uint32_t)(cache->Hkv * (cache->Dh * (cache->k_exp ? 1 : 2) / 16)));
+  a.N = N;
+  a.copies = copies;
+  HIPCHECK(launch_page_copy(a, stream));
+  return WAM_OK;
+}
+
+wam_status wam_page_collect(const wam_page_collect_desc* desc, const int32_t* cache_len, const int32_t* held,
+                            const int32_t* block_table, int32_t* free_list, int32_t* held_out, int32_t* n_free_out,
+                            int32_t* status, hipStream_t stream) {
+  CHECK(desc, WAM_EINVAL, "desc is NULL");
+  const wam_page_collect_desc& d = *desc;
+  CHECK(d.R <= WAM_PLAN_MAX_REQUESTS, WAM_EUNSUPPORTED, "R=%d exceeds %d", d.R, WAM_PLAN_MAX_REQUESTS);
+  TRY(check_page_size(d.page_size, d.n_pages));
+  CHECK(d.n_pages <= WAM_COLLECT_MAX_PAGES, WAM_EUNSUPPORTED, "n_pages=%d exceeds %d", d.n_pages, WAM_COLLECT_MAX_PAGES);
+  TRY(check_table(d.R, d.max_pages, d.table_stride, block_table));
+  if (d.R > 0) {
+    TRY(need_ints(cache_len, "cache_len"));
+    TRY(need_ints(held, "held"));
+    TRY(need_ints(held_out, "held_out"));
+  }
+  if (d.n_pages > 0) TRY(need_ints(free_list, "free_list"));
+  TRY(need_ints(n_free_out, "n_free_out"));
+  TRY(need_ints(status, "status"));
+  const Ints all[] = {{"free_list", free_list, d.n_pages, 1, 0, true},
+                      {"held_out", held_out, d.R, 1, 0, true},
+                      {"n_free_out", n_free_out, 1, 1, 0, true},
+                      {"status", status, 2, 1, 0, true},
+                      {"block_table", block_table, d.max_pages, d.R, d.table_stride, false},
+                      {"cache_len", cache_len, d.R, 1, 0, false},
+                      {"held", held, d.R, 1, 0, false}};
+  TRY(check_apart(all));
+  PageCollectArgs a{};
+  a.d = d;
+  a.ps = fast_div((uint32_t)d.page_size);
+  a.cache_len = cache_len; a.held = held; a.table = block_table;
+  a.free_list = free_list; a.held_out = held_out; a.n_free_out = n_free_out; a.status = status;
+  HIPCHECK(launch_page_collect(a, stream));
+  return WAM_OK;
+}
+
+wam_status wam_cache_compact(const wam_cache_compact_desc* desc, const wam_paged_cache* cache, const int32_t* block_table,
+                             const int32_t* q_start, const int32_t* q_len, const int32_t* kv_len, const int32_t* keep,
+                             const int32_t* n_keep, hipStream_t stream) {
+  CHECK(desc && cache, WAM_EINVAL, "desc or cache is NULL");
+  const wam_cache_compact_desc& d = *desc;
+  TRY(check_cache(*cache));
+  CHECK(d.T >= 0, WAM_EINVAL, "T=%d is negative", d.T);
+  TRY(check_table(d.R, d.max_pages, d.table_stride, block_table));
+  if (d.R == 0 || d.T == 0 || d.max_pages == 0 || cache->n_pages == 0) return WAM_OK;
+  TRY(need_ints(q_start, "q_start"));
+  TRY(opt_ints(q_len, "q_len"));
+  TRY(need_ints(kv_len, "kv_len"));
+  TRY(need_ints(keep, "keep"));
+  TRY(need_ints(n_keep, "n_keep"));
+  TRY(check_launch(2 * (int64_t)d.R * cache->Hkv * 256));
+  CacheCompactArgs a{};
+  a.c = *cache;
+  a.ps = fast_div((uint32_t)cache->page_size);
+  a.by_heads = fast_div((uint32_t)cache->Hkv);
+  a.R = d.R; a.T = d.T; a.max_pages = d.max_pages; a.table_stride = d.table_stride;
+  a.table = block_table; a.q_start = q_start; a.q_len = q_len; a.kv_len = kv_len; a.keep = keep; a.n_keep = n_keep;
+  HIPCHECK(launch_cache_compact(a, stream));
+  return WAM_OK;
+}
+
+size_t wam_attn_tree_workspace_bytes(const wam_attn_tree_desc* desc, const wam_paged_cache* cache) {
+  if (!desc || !cache || check_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv) != WAM_OK) return 0;
+  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv), desc->T, desc->Hq, cache->Dh);
+}
+
+wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* cache, const void* q,
+                         const int32_t* block_table, const int32_t* q_start, const int32_t* q_len,
+                         const int32_t* kv_len, const uint32_t* mask, void* o, void* ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  CHECK(desc && cache, WAM_EINVAL, "desc or cache is NULL");
+  const wam_attn_tree_desc& d = *desc;
+  CHECK(d.mask_words >= 0 && d.mask_stride >= d.mask_words && d.mask_stride <= INT64_MAX / 8 / ((int64_t)(d.T < 0 ? 0 : d.T) + 1),
+        WAM_EINVAL, "mask_stride=%lld must be >= mask_words=%d >= 0", (long long)d.mask_stride, d.mask_words);
+  if (d.R > 0 && d.T > 0 && d.mask_words > 0) TRY(need_ints(mask, "mask"));
+  RaggedArgs a{};
+  a.mask = mask;
+  a.mask_stride = d.mask_stride;
+  a.mask_words = d.mask_words;
+  const wam_attn_paged_desc p{d.R, d.T, d.Hq, d.max_pages, d.max_kv, 0, d.table_stride, d.q_tok_stride, d.o_tok_stride, d.scale};
+  return run_paged(p, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, launch_attn_tree, stream);
+}
+
+size_t wam_verify_tree_workspace_bytes(const wam_verify_tree_desc* desc) {
+  if (!desc || check_verify(*desc) != WAM_OK) return 0;
+  return verify_ws_bytes(*desc);
+}
+
+wam_status wam_verify_tree(const wam_verify_tree_desc* desc, const float* p, const float* q, const int32_t* tokens,
+                           const int32_t* parent, const float* u, const float* u_next, const int32_t* q_start,
+                           const int32_t* q_len, const int32_t* kv_len, int32_t* path, int32_t* n_path,
+                           int32_t* next_token, int32_t* cache_len, void* ws, size_t ws_bytes, hipStream_t stream) {
+  CHECK(desc, WAM_EINVAL, "desc is NULL");
+  const wam_verify_tree_desc& d = *desc;
+  TRY(check_verify(d));
+  CHECK(!d.drawn == !q, WAM_EINVAL, "q must be given where drawn is 1 and only there");
+  CHECK(!kv_len == !cache_len, WAM_EINVAL, "kv_len and cache_len must be given both or neither");
+  if (d.R == 0) return WAM_OK;
+  if (d.T > 0) {
+    TRY(need_ints(p, "p"));
+    TRY(opt_ints(q, "q"));
+    TRY(need_ints(tokens, "tokens"));
+    TRY(need_ints(parent, "parent"));
+    TRY(need_ints(u, "u"));
+    TRY(need_ints(path, "path"));
+  }
+  TRY(need_ints(u_next, "u_next"));
+  TRY(need_ints(q_start, "q_start"));
+  TRY(opt_ints(q_len, "q_len"));
+  TRY(opt_ints(kv_len, "kv_len"));
+  TRY(need_ints(n_path, "n_path"));
+  TRY(need_ints(next_token, "next_token"));
+  TRY(opt_ints(cache_len, "cache_len"));
+  const auto ints = [](const float* x) { return reinterpret_cast<const int32_t*>(x); };
+  const Ints all[] = {{"path", path, d.T, 1, 0, true},
+                      {"n_path", n_path, d.R, 1, 0, true},
+                      {"next_token", next_token, d.R, 1, 0, true},
+                      {"cache_len", cache_len, d.R, 1, 0, true},
+                      {"p", ints(p), d.V, d.T, d.p_stride, false},
+                      {"q", ints(q), d.V, d.T, d.q_stride, false},
+                      {"tokens", tokens, d.T, 1, 0, false},
+                      {"parent", parent, d.T, 1, 0, false},
+                      {"u", ints(u), d.T, 1, 0, false},
+                      {"u_next", ints(u_next), d.R, 1, 0, false},
+                      {"q_start", q_start, (int64_t)d.R + 1, 1, 0, false},
+                      {"q_len", q_len, d.R, 1, 0, false},
+                      {"kv_len", kv_len, d.R, 1, 0, false}};
+  TRY(check_apart(all));
+  TRY(check_ws(ws, ws_bytes, verify_ws_bytes(d)));
+  VerifyArgs a{};
+  a.d = d;
+  a.p = p; a.q = q; a.u = u; a.u_next = u_next;
+  a.tokens = tokens; a.parent = parent; a.q_start = q_start; a.q_len = q_len; a.kv_len = kv_len;
+  a.path = path; a.n_path = n_path; a.next_token = next_token; a.cache_len = cache_len;
+  a.slices = verify_slices(d);
+  a.rounds = verify_rounds(d);
+  a.by_slices = fast_div((uint32_t)a.slices);
+  a.state = static_cast<VerifyState*>(ws);
+  a.sums = reinterpret_cast<double*>(a.state + (int64_t)a.rounds * d.R);
+  HIPCHECK(launch_verify_tree(a, stream));
+  return WAM_OK;
+}
+
+wam_status wam_tree_mask(const int32_t* parent, int32_t n, int32_t words, uint32_t* mask) {
+  CHECK(n >= 0 && words >= 0 && n <= 32 * (int64_t)words, WAM_EINVAL, "n=%d nodes do not fit %d words", n, words);
+  CHECK(n == 0 || (parent && mask), WAM_EINVAL, "parent or mask is NULL");
+  for (int32_t i = 0; i < n; ++i)
+    CHECK(parent[i] >= -1 && parent[i] < i, WAM_EINVAL, "parent[%d]=%d must be -1 or a node before it", i, parent[i]);
+  for (int32_t i = 0; i < n; ++i) {
+    uint32_t* row = mask + (int64_t)i * words;
+    for (int32_t w = 0; w < words; ++w) row[w] = parent[i] < 0 ? 0u : mask[(int64_t)parent[i] * words + w];
+    row[i >> 5] |= 1u << (i & 31);
+  }
   return WAM_OK;
 }
 

@@ -326,7 +326,71 @@ struct RaggedArgs {
   int32_t R, T, Hq, Hkv, Dh, max_k, n_pages, S;
   FastDiv ps, group, chunk;  // page size, query heads per KV head, chunk (d = 0: none)
   float c, v_scale;  // c: softmax scale * log2(e)
+  const uint32_t* mask;  // tree: rows of mask_words words, a bit for each of the request's new tokens
+  int64_t mask_stride;
+  int32_t mask_words;
 };
 hipError_t launch_attn_ragged(const RaggedArgs& a, const RaggedPlan& p, void* ws, hipStream_t s);
+// over pages, the new tokens visible by a.mask
+hipError_t launch_attn_tree(const RaggedArgs& a, const RaggedPlan& p, void* ws, hipStream_t s);
+
+// Requests that branch.
+struct PageForkArgs {
+  wam_page_fork_desc d;
+  FastDiv ps;
+  const int32_t *src, *dst, *first, *len, *held, *n_free, *free_list;
+  int32_t *table, *held_out, *n_free_out, *copies, *status;
+};
+hipError_t launch_page_fork(const PageForkArgs& a, hipStream_t s);
+struct PageCopyArgs {
+  wam_paged_cache c;
+  FastDiv by_blocks, by_row;  // workgroups of a copy, 16-byte chunks of K of a token
+  int32_t N;
+  const int32_t* copies;
+};
+// workgroups of a copy: 1024 chunks of K (and V) each
+inline int64_t page_copy_blocks(const wam_paged_cache& c) {
+  return ((int64_t)c.page_size * c.Hkv * (c.Dh * (c.k_exp ? 1 : 2) / 16) + 1023) / 1024;
+}
+hipError_t launch_page_copy(const PageCopyArgs& a, hipStream_t s);
+struct PageCollectArgs {
+  wam_page_collect_desc d;
+  FastDiv ps;
+  const int32_t *cache_len, *held, *table;
+  int32_t *free_list, *held_out, *n_free_out, *status;
+};
+hipError_t launch_page_collect(const PageCollectArgs& a, hipStream_t s);
+struct CacheCompactArgs {
+  wam_paged_cache c;
+  FastDiv ps, by_heads;
+  int32_t R, T, max_pages;
+  int64_t table_stride;
+  const int32_t *table, *q_start, *q_len, *kv_len, *keep, *n_keep;
+};
+hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t s);
+
+// Verification of drafted trees: nodes of a request that are looked at, vocabulary entries of a workgroup, passes over the
+// vocabulary by all workgroups (a further one is done by a request's last workgroup alone).
+constexpr int VERIFY_SLICE = 4096, VERIFY_ROUNDS = 2;
+struct VerifyState {
+  double c, s;
+  int32_t cur, count, next, done, round, pad[3];
+};
+struct VerifyArgs {
+  wam_verify_tree_desc d;
+  const float *p, *q, *u, *u_next;
+  const int32_t *tokens, *parent, *q_start, *q_len, *kv_len;
+  int32_t *path, *n_path, *next_token, *cache_len;
+  VerifyState* state;  // [rounds][R]
+  double* sums;        // [rounds][R][slices]
+  int32_t slices, rounds;
+  FastDiv by_slices;
+};
+inline int verify_rounds(const wam_verify_tree_desc& d) { return d.drawn ? VERIFY_ROUNDS : 1; }
+inline int verify_slices(const wam_verify_tree_desc& d) { return (d.V + VERIFY_SLICE - 1) / VERIFY_SLICE; }
+inline size_t verify_ws_bytes(const wam_verify_tree_desc& d) {
+  return (size_t)verify_rounds(d) * d.R * (sizeof(VerifyState) + 8 * (size_t)verify_slices(d));
+}
+hipError_t launch_verify_tree(const VerifyArgs& a, hipStream_t s);
 
 }  // namespace wam
