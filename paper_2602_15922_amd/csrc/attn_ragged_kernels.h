@@ -41,6 +41,7 @@ struct Parts {
   float* ml;  // [row][splits][2]: reference and sum
   float* o;   // [row][splits][Dh]
   int splits, split_keys, tiles;
+  int turns;  // tree, tile kernel: parts and requests in turn over the XCDs, as the streaming kernel has them
   FastDiv by_splits, by_tiles, by_heads;
 };
 
@@ -107,6 +108,23 @@ WAM_DEV uint32_t tree_bits(const RaggedArgs& a, const Req& q, int tok, int key) 
   const uint32_t lo = word(w), hi = word(w + 1), b = __builtin_amdgcn_alignbit(hi, lo, (int)i & 31);
   const int left = q.keys - key;
   return left >= 32 ? b : (left <= 0 ? 0u : b & ((1u << left) - 1));
+}
+
+// The same for 64 keys in two steps: the three words around them, and their bits in order.
+WAM_DEV void tree_words(const RaggedArgs& a, const Req& q, int tok, int key, uint32_t* x) {
+  const int w = (int)(((int64_t)key - q.kv + q.n) >> 5);
+  const uint32_t* row = a.mask + (int64_t)(q.q0 + tok) * a.mask_stride;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) x[k] = w + k < 0 ? ~0u : (w + k < a.mask_words ? row[w + k] : 0u);
+}
+WAM_DEV void tree_align(const Req& q, int key, const uint32_t* x, uint32_t* bits) {
+  const int sh = (int)((int64_t)key - q.kv + q.n) & 31;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int left = q.keys - key - 32 * k;
+    const uint32_t b = __builtin_amdgcn_alignbit(x[k + 1], x[k], sh);
+    bits[k] = left >= 32 ? b : (left <= 0 ? 0u : b & ((1u << left) - 1));
+  }
 }
 
 // page of the 16 keys from `key` on (a multiple of 16), -1 where there is none (or the table ends)
@@ -685,7 +703,7 @@ WAM_DEV void tile_arrived() {
 // False, and nothing is written: V of keys that only some of the rows see holds values that are not finite.
 template <int DH, int KEYS, bool FP8, int GROUPS>
 WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
-                       bool whole, int start, int end, int meta, bf16* smem_all) {
+                       bool whole, int start, int end, int meta, bf16* smem_all, int* odd) {
   constexpr int KS = DH / 16, MT = DH / 32, TILE = 2 * BN * DH;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int w = uniform(tid >> 6) & 3, grp = GROUPS == 1 ? 0 : uniform(tid >> 8);
@@ -730,13 +748,37 @@ WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
     f.load(a, q, smem + cur * TILE, key, pg, nv, hk, w, lane);
   };
   bool bad = false;
+  // tree: the words of the row's mask around a tile's 64 keys, fetched behind the tile's own loads (and so there when it is)
+  uint32_t words[3];
+  const auto fetch_words = [&](int t) {
+    if constexpr (KEYS == TREE) {
+      if (t * BN + BN > kmin) tree_words(a, q, tok, t * BN, words);
+    }
+  };
   // this group's tiles: t0 + grp, then every GROUPS-th; two at a time, one per buffer
   if (t0 + grp < nt) {
     fetch(t0 + grp, 0, t0 + 16);
+    fetch_words(t0 + grp);
     f.store(smem, w, lane);
   }
   tile_arrived();
-  for (int wb = t0; wb < nt; wb += 16) {
+  const bool idle = KEYS == TREE && m0 + 32 * w >= rows;  // no rows: loads for the others alone
+  if (KEYS == TREE && idle) {
+    for (int wb = t0; wb < nt; wb += 16) {
+      meta_next = page_of<KEYS>(a, r, (wb + 16) * BN + 16 * lane);
+      for (int tb = wb; tb < (wb + 16 < nt ? wb + 16 : nt); tb += GROUPS) {
+        const int t = tb + grp, cur = (tb - t0) / GROUPS & 1;
+        if (t + GROUPS < nt) {
+          fetch(t + GROUPS, cur ^ 1, wb + 16);
+          f.store(smem + (cur ^ 1) * TILE, w, lane);
+        }
+        tile_arrived();
+        if (__any(*odd != 0)) bad = true;
+      }
+      meta = meta_next;
+    }
+  }
+  for (int wb = t0; wb < (idle ? t0 : nt); wb += 16) {
     const int we = wb + 16 < nt ? wb + 16 : nt;
     meta_next = page_of<KEYS>(a, r, (wb + 16) * BN + 16 * lane);
     // (groups past the end count as present: the rows' prefixes hide them)
@@ -747,22 +789,40 @@ WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
       const int t = tb + grp;
       if (GROUPS == 1 || t < nt) {
         const int groups = (int)(there >> (4 * (t - wb))) & 15;
-        uint32_t bits[2];
-        if constexpr (KEYS == TREE && decltype(mask)::value) {  // (before the next tile's loads, so as not to wait for them)
+        uint32_t bits[2] = {~0u, ~0u};
+        if constexpr (KEYS == TREE && decltype(mask)::value) {
+          if (t * BN + BN > kmin) tree_align(q, t * BN, words, bits);
 #pragma unroll
-          for (int nt2 = 0; nt2 < 2; ++nt2)
-            bits[nt2] = (tree_bits(a, q, tok, t * BN + 32 * nt2) &
-                         ((groups >> (2 * nt2) & 1 ? 0xffffu : 0u) | (groups >> (2 * nt2 + 1) & 1 ? 0xffff0000u : 0u))) >> (4 * hh);
+          for (int i = 0; i < 2; ++i)
+            bits[i] &= (groups >> (2 * i) & 1 ? 0xffffu : 0u) | (groups >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
         }
-        if (t + GROUPS < nt) fetch(t + GROUPS, cur ^ 1, wb + 16);
+        if (t + GROUPS < nt) {
+          fetch(t + GROUPS, cur ^ 1, wb + 16);
+          fetch_words(t + GROUPS);
+        }
         const char* Ks = reinterpret_cast<const char*>(smem + cur * TILE);
         // (keys that the first row does not see: the same answer in every wavefront of the group)
-        if (decltype(mask)::value && kmin < end && t * BN + BN > kmin && any_not_finite<DH>(Ks + BN * DH * 2, lane)) bad = true;
-        ragged_tile<DH, KEYS, decltype(mask)::value>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend, groups,
-                                                     bits, hh);
+        if constexpr (KEYS == TREE && decltype(mask)::value) {
+          // (the rows of this wavefront see some of the tile's keys and not others)
+          if (__any((bits[0] | bits[1]) != 0) && __any((bits[0] & bits[1]) != ~0u) && any_not_finite<DH>(Ks + BN * DH * 2, lane))
+            *odd = 1;
+        }
+        if (KEYS != TREE && decltype(mask)::value && kmin < end && t * BN + BN > kmin && any_not_finite<DH>(Ks + BN * DH * 2, lane)) bad = true;
+        if constexpr (KEYS == TREE && decltype(mask)::value) {
+          // (a tile of which the wavefront's rows see nothing takes no work)
+          if (__any((bits[0] | bits[1]) != 0)) {
+            bits[0] >>= 4 * hh;
+            bits[1] >>= 4 * hh;
+            ragged_tile<DH, KEYS, true>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend, groups, bits, hh);
+          }
+        } else {
+          ragged_tile<DH, KEYS, decltype(mask)::value>(Ks, qf, acc, m_ref, l_part, kofs, vofs, c, thr, t * BN, row_kend, groups,
+                                                       bits, hh);
+        }
         if (t + GROUPS < nt) f.store(smem + (cur ^ 1) * TILE, w, lane);
       }
       tile_arrived();
+      if (KEYS == TREE && decltype(mask)::value && __any(*odd != 0)) bad = true;  // (any wavefront's)
       tb += GROUPS;
     };
     while (tb + 2 * GROUPS <= plain) {
@@ -890,7 +950,7 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, int block, Work& k)
   const int lane = threadIdx.x & 63;
   k.G = (int)a.group.d;
   int x;
-  if (SHIFT == 7) {
+  if (SHIFT == 7 && !(KEYS == TREE && pt.turns)) {
     // rows share keys with their neighbours: each XCD a contiguous range of (row tile, head) pairs
     const int nblk = gridDim.x, bi = block, xcd = bi & 7, per = nblk >> 3, rem = nblk & 7;
     const int lid = xcd * per + (xcd < rem ? xcd : rem) + (bi >> 3);
@@ -933,11 +993,17 @@ template <int DH, int KEYS, bool FP8, int GROUPS>
 __global__ __launch_bounds__(NT * GROUPS, DH == 64 ? 3 : 2) void ragged_tile_kernel(const RaggedArgs a, const Parts pt) {
   __shared__ __attribute__((aligned(16))) bf16 smem[GROUPS * 4 * BN * DH];
   static_assert(RAGGED_ROWS == 128, "2^7 rows");
+  int* odd = nullptr;
+  if constexpr (KEYS == TREE) {
+    __shared__ int found;
+    odd = &found;
+    if (threadIdx.x == 0) found = 0;  // (before the first tile's barrier)
+  }
   Work k;
   if (!find_work<KEYS, 7>(a, pt, blockIdx.x, k)) return;
   int last = k.m0 + 1;  // streamed: the rows m0 .. last - 1, 32 at a time
   if (GROUPS == 2 || k.q.n * k.G > RAGGED_STREAM) {
-    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem))
+    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem, odd))
       return;
     int block = blockIdx.x;  // (found anew, so that nothing is kept for it: two samples' 3152 rows 1861 -> 1831 us)
     asm volatile("" : "+s"(block) : : "memory");
@@ -1072,10 +1138,11 @@ hipError_t launch(const RaggedArgs& a, const Parts& pt, const RaggedPlan& p, hip
 }
 
 inline Parts make_parts(const RaggedArgs& a, const RaggedPlan& p, void* ws) {
-  Parts pt;
+  Parts pt{};
   pt.ml = static_cast<float*>(ws);
   pt.o = reinterpret_cast<float*>(static_cast<char*>(ws) + ragged_ml_bytes(p, a.T, a.Hq));
   pt.splits = p.splits;
+  pt.turns = p.turns;
   pt.split_keys = p.split_keys;
   pt.tiles = (int)ragged_tiles(a.R, a.T, a.Hq, a.Hkv, p.rows);
   pt.by_splits = fast_div(p.splits);

@@ -133,7 +133,8 @@ wam_status check_ws(const void* ws, size_t have, size_t need) {
 // attention over pages; a holds what says which keys a row sees
 wam_status run_paged(const wam_attn_paged_desc& d, const wam_paged_cache& c, const void* q, const int32_t* block_table,
                      const int32_t* q_start, const int32_t* q_len, const int32_t* kv_len, void* o, void* ws, size_t ws_bytes,
-                     RaggedArgs& a, hipError_t (*launch)(const RaggedArgs&, const RaggedPlan&, void*, hipStream_t),
+                     RaggedArgs& a, RaggedPlan (*plan)(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t),
+                     hipError_t (*launch)(const RaggedArgs&, const RaggedPlan&, void*, hipStream_t),
                      hipStream_t stream) {
   TRY(check_cache(c));
   TRY(check_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv));
@@ -147,7 +148,7 @@ wam_status run_paged(const wam_attn_paged_desc& d, const wam_paged_cache& c, con
   TRY(opt_ints(q_len, "q_len"));
   TRY(need_ints(kv_len, "kv_len"));
   if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
-  const RaggedPlan p = plan_ragged(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
+  const RaggedPlan p = plan(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
   TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
   TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, c.Hkv) * 256 * p.groups));
   a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
@@ -301,7 +302,7 @@ wam_status wam_attn_paged(const wam_attn_paged_desc* desc, const wam_paged_cache
   CHECK(desc && cache, WAM_EINVAL, "desc or cache is NULL");
   RaggedArgs a{};
   if (desc->chunk > 0) a.chunk = fast_div((uint32_t)desc->chunk);
-  return run_paged(*desc, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, launch_attn_ragged, stream);
+  return run_paged(*desc, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, plan_ragged, launch_attn_ragged, stream);
 }
 
 size_t wam_attn_cross_workspace_bytes(const wam_attn_cross_desc* desc) {
@@ -473,7 +474,7 @@ wam_status wam_cache_compact(const wam_cache_compact_desc* desc, const wam_paged
 
 size_t wam_attn_tree_workspace_bytes(const wam_attn_tree_desc* desc, const wam_paged_cache* cache) {
   if (!desc || !cache || check_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv) != WAM_OK) return 0;
-  return ragged_ws_bytes(plan_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv), desc->T, desc->Hq, cache->Dh);
+  return ragged_ws_bytes(plan_tree(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv), desc->T, desc->Hq, cache->Dh);
 }
 
 wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* cache, const void* q,
@@ -490,7 +491,7 @@ wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* 
   a.mask_stride = d.mask_stride;
   a.mask_words = d.mask_words;
   const wam_attn_paged_desc p{d.R, d.T, d.Hq, d.max_pages, d.max_kv, 0, d.table_stride, d.q_tok_stride, d.o_tok_stride, d.scale};
-  return run_paged(p, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, launch_attn_tree, stream);
+  return run_paged(p, *cache, q, block_table, q_start, q_len, kv_len, o, ws, ws_bytes, a, plan_tree, launch_attn_tree, stream);
 }
 
 size_t wam_verify_tree_workspace_bytes(const wam_verify_tree_desc* desc) {

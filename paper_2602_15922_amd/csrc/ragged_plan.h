@@ -14,6 +14,7 @@ struct RaggedPlan {
   int groups = 1;          // groups of four wavefronts of a workgroup of the tile kernel
   int splits = 1;          // workgroups along the key axis, at most
   int split_keys = 0;      // keys of each (a multiple of 128)
+  int turns = 0;           // tile kernel of trees: parts and requests in turn over the XCDs
 };
 
 // From what the host knows: R requests with T rows together (packed or padded), at most max_k keys.
@@ -70,11 +71,36 @@ inline int64_t ragged_tiles(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int r
   return (T * (Hq / Hkv) + rows - 1) / rows + R - 1;
 }
 
-// Workgroups of the launch (256 threads per group of four wavefronts): one per row tile, part and KV head; of the streaming
-// kernel, row tiles and parts in eights, one to each XCD.
+// Trees of new tokens (over pages): a request has some tens of rows more often than one or thousands.
+inline RaggedPlan plan_tree(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t Dh, int64_t max_k) {
+  RaggedPlan p = plan_ragged(R, T, Hq, Hkv, Dh, max_k);
+  const int64_t rows = T * (Hq / Hkv);
+  if (rows <= 16 * R || rows > 4 * RAGGED_ROWS * R || R <= 1) return p;
+  // 17 to 512 rows on average: the tile kernel, which streams requests of up to 32 rows and reads the keys of the others once
+  // for 128 rows (48 requests of 5 to 60 rows, E4M3, 1048-32012 keys: 240 us; the streaming kernel with 32 rows 267).  Parts of
+  // 2048 keys unless there are thousands of workgroups without, in turn over the XCDs: 16 requests of 96 to 256 rows, 8 heads,
+  // 332-16064 keys at 1024, 1536, 2048, 4096 keys 123, 127, 105, 160 us (by row tile and head on the XCDs 234, 225, 224, 202);
+  // the 48 requests 264, 259, 240, 257 us.
+  p = RaggedPlan{};
+  const int64_t per = (rows + p.rows - 1) / p.rows, tiles = (R < T ? R : T) > per ? (R < T ? R : T) : per;
+  int64_t n = 8192 / (tiles * Hkv > 0 ? tiles * Hkv : 1);
+  const int64_t by_keys = (max_k + 2047) / 2048;
+  if (n > RAGGED_MAX_SPLITS) n = RAGGED_MAX_SPLITS;
+  if (n > by_keys) n = by_keys;
+  if (n < 1) n = 1;
+  const int64_t keys = ((max_k + n - 1) / n + 127) / 128 * 128;
+  p.split_keys = (int)(keys < 128 ? 128 : keys);
+  p.splits = (int)((max_k + p.split_keys - 1) / p.split_keys);
+  if (p.splits < 1) p.splits = 1;
+  p.turns = p.splits > 1 && ragged_tiles(R, T, Hq, Hkv, p.rows) * p.splits >= 16;
+  return p;
+}
+
+// Workgroups of the launch (256 threads per group of four wavefronts): one per row tile, part and KV head; where they go
+// in turn over the XCDs (the streaming kernel, some trees), row tiles and parts in eights, one to each XCD.
 inline int64_t ragged_blocks(const RaggedPlan& p, int64_t R, int64_t T, int64_t Hq, int64_t Hkv) {
   const int64_t parts = ragged_tiles(R, T, Hq, Hkv, p.rows) * p.splits;
-  return (p.rows == RAGGED_ROWS ? parts : (parts + 7) / 8 * 8) * Hkv;
+  return (p.rows == RAGGED_ROWS && !p.turns ? parts : (parts + 7) / 8 * 8) * Hkv;
 }
 
 // Workspace: per row and split the reference and the sum (8 bytes), then Dh partial outputs.

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 import branch_ref
-from test_paged_abi_host import FP8, cache, lib
+from test_paged_abi_host import cache, lib
 
 
 def refused(status_says, status, says):
@@ -129,15 +129,6 @@ def test_tree_refusals(bad, desc, ptrs, status, says):
         setattr(d, k, v)
     p = dict(q=4096, block_table=4096, q_start=4096, q_len=None, kv_len=4096, mask=4096, o=8192, ws=1 << 20) | ptrs
     refused((L.wam_attn_tree(C.byref(d), C.byref(c), *p.values(), 1 << 40, None), L.wam_last_error().decode()), status, says)
-
-
-def test_tree_workspace_is_the_paged_attentions():
-    w, b, _ = lib()
-    for f in ({}, FP8):
-        for R, T, Hq, kv in ((1, 16, 4, 5000), (9, 40, 8, 700), (0, 0, 4, 100), (2, 300, 4, 90000)):
-            c = cache(**f)
-            assert w.wam_attn_tree_workspace_bytes(c, R, T, Hq, kv) == w.wam_attn_paged_workspace_bytes(c, R, T, Hq, kv)
-    assert w.wam_attn_tree_workspace_bytes(cache(), -1, 5, 4, 100) == 0
 
 
 # ---- verification ----
