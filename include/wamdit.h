@@ -702,11 +702,10 @@ wam_status wam_page_collect(const wam_page_collect_desc* desc, const int32_t* ca
 
 /* wam_cache_compact — the rows of the new tokens that a request keeps, moved together (one layer's cache).
  *
- * Request r's n = q_len[r] new tokens are the last of its kv_len[r]; it keeps m = n_keep[r] of them, numbers keep[q_start[r] + i]
- * in [0, n), i < m, ascending.  Row kv_len - n + keep[i] of its K, V and exponents goes to kv_len - n + i, all of them as they
+ * Request r's n = q_len[r] new tokens are the last of its kv_len[r]; it keeps m = n_keep[r] of them, numbers keep[q_start[r] + i],
+ * i < m, ascending.  Row kv_len - n + keep[i] of its K, V and exponents goes to kv_len - n + i, all of them as they
  * were before the call; the rows past kv_len - n + m keep what they hold.  (The path of wam_verify_tree is such a list.)
- * A number outside [0, n) and rows of absent pages are left out.  Numbers that do not ascend leave the rows that they name with values of
- * some of them (the same at every call).  The rows' pages may belong to no other request. */
+ * Numbers outside (i, n) (in a list that does not ascend, those below their place) and rows of absent pages are left out. The rows' pages may belong to no other request. */
 typedef struct {
   int32_t R, T, max_pages;
   int64_t table_stride;

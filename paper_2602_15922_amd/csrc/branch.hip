@@ -27,7 +27,8 @@ WAM_DEV int wave_scan(int v) {
 // ---------------------------------------------------------------------------------
 // Fork.  Every workgroup finds in LDS which forks hold (the first to name a destination, which holds no page) and how many
 // of those before each need a page of their own; so one launch does it and none waits for another.  Rows that are
-// written belong to requests without pages and rows that are read to requests with some, so no order matters.
+// written belong to requests without pages and rows that are read to requests with some, so no order matters.  Bound by
+// latency (starts -> lengths -> table): 8 forks of 198 pages 3.0 us, 256 of up to 63 pages 4.9.
 // ---------------------------------------------------------------------------------
 constexpr int FORK_NT = 256;
 
@@ -137,7 +138,8 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
 }
 
 // ---------------------------------------------------------------------------------
-// Copies of pages' first rows: 16-byte chunks of K and V in the order of the rows, four of each per thread on their way.
+// Copies of pages' first rows: 16-byte chunks of K and V in the order of the rows, four of each per thread on their way.  Bound
+// by memory: 256 copies of 0 to 127 rows, 16 heads of 128, 54.6 us for 247 MB (4.5 TB/s; a large copy reaches 4.85).
 // ---------------------------------------------------------------------------------
 constexpr int COPY_NT = 256, COPY_PER = 4;
 
@@ -173,10 +175,14 @@ __global__ __launch_bounds__(COPY_NT) void page_copy_kernel(const PageCopyArgs a
 }
 
 // ---------------------------------------------------------------------------------
-// Collect.  Every workgroup marks the pages that the requests keep in a bit map in LDS (n_pages bits, at most 128 KB), a
-// wavefront per row of the table; then it knows how many free pages lie below its share of the pool and lists its own.
+// Collect.  Every workgroup marks the pages that the requests keep in LDS, a byte each (plain stores: lanes that meet store
+// the same), so it knows how many free pages lie below its share of the pool and lists its own; one launch does
+// it and none waits for another.  Pools of more bytes than LDS has go by segments, from the first on.
+// Bound by the instructions that one CU issues for all marks (16 wavefronts, 4 cycles each): so no lane is masked off, 8 rows' first 64
+// entries are on their way at once and then a longer row's, 512 at a time.  1000 requests that keep 0 to 667 pages, 144700 pages: 28 us;
+// with lanes masked 40, a wavefront per row with atomic marks of a bit 44; 12 requests, 2224 pages 8.
 // ---------------------------------------------------------------------------------
-constexpr int COLLECT_NT = 1024;
+constexpr int COLLECT_NT = 1024, COLLECT_SMALL = 32 << 10, COLLECT_LARGE = 152 << 10;
 
 WAM_DEV int kept_pages(const PageCollectArgs& a, int r, bool* bad) {
   const int c = a.cache_len[r], h = a.held[r], len = c < 0 ? 0 : c, held = clampi(h, 0, a.d.max_pages);
@@ -185,141 +191,210 @@ WAM_DEV int kept_pages(const PageCollectArgs& a, int r, bool* bad) {
   return need < held ? need : held;
 }
 
-template <int WORDS>  // n_pages <= 32 WORDS
-__global__ __launch_bounds__(COLLECT_NT) void page_collect_kernel(const PageCollectArgs a) {
-  __shared__ uint32_t used[WORDS];
-  __shared__ int wave[COLLECT_NT / 64], miss[COLLECT_NT / 64];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n_pages = a.d.n_pages, words = (n_pages + 31) >> 5;
-  for (int i = tid; i < words; i += COLLECT_NT) used[i] = 0;
+// sum over the workgroup, the same in every thread (tmp: an int per wavefront; barriers inside)
+WAM_DEV int block_sum(int v, int* tmp) {
+  // (the wavefronts' sums: a lane each)
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k, 64);
   __syncthreads();
-  int missing = 0, wrong = 0;
-  for (int r = w; r < a.d.R; r += COLLECT_NT / 64) {
-    bool bad;
-    const int kept = kept_pages(a, r, &bad);
-    const int32_t* row = a.table + (int64_t)r * a.d.table_stride;
-    for (int j = lane; j < kept; j += 64) {
-      const int p = row[j];
-      if ((unsigned)p < (unsigned)n_pages) atomicOr(&used[p >> 5], 1u << (p & 31));
-      else ++missing;
+  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+  __syncthreads();
+  int sum = tmp[threadIdx.x & 15];
+#pragma unroll
+  for (int k = 1; k < 16; k <<= 1) sum += __shfl_xor(sum, k, 64);
+  return sum;
+}
+
+template <int SEGMENT>  // pages whose marks fit at once, a multiple of 16
+__global__ __launch_bounds__(COLLECT_NT) void page_collect_kernel(const PageCollectArgs a, int share) {
+  constexpr int WAVES = COLLECT_NT / 64;
+  __shared__ __attribute__((aligned(16))) uint8_t used[SEGMENT + 16];  // 1: kept (or past the pool)
+  __shared__ int tmp[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n_pages = a.d.n_pages;
+  const bool last = blockIdx.x == gridDim.x - 1;  // counts all pages, and the status
+  const int lo = (int)blockIdx.x * share, hi = last || n_pages - lo < share ? n_pages : lo + share;
+  const int mine = a.d.R > w ? (a.d.R - w + WAVES - 1) / WAVES : 0;  // rows w + 16 i: 64 at a time, a lane each
+  int at = 0, total = 0, missing = 0, wrong = 0;                     // at: free pages below what is listed next
+  for (int seg = 0; seg == 0 || seg < hi; seg += SEGMENT) {
+    const int pages = n_pages - seg < SEGMENT ? n_pages - seg : SEGMENT, groups = (pages + 15) >> 4;
+    const auto lengths = [&](int base) {
+      const int i = base + lane, r = w + WAVES * i;
+      if (i >= mine) return 0;
+      bool bad;
+      const int kept = kept_pages(a, r, &bad);
+      if (last && seg == 0) {
+        wrong += bad;
+        a.held_out[r] = kept;
+      }
+      return kept;
+    };
+    int kept = lengths(0);
+    for (int i = tid; i < groups; i += COLLECT_NT) {
+      u32x4v z = {0, 0, 0, 0};
+      if (16 * i + 16 > pages)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (16 * i + e >= pages) z[e >> 2] |= 1u << (8 * (e & 3));
+      *reinterpret_cast<u32x4v*>(used + 16 * i) = z;
     }
-    if (lane == 0) {
-      wrong += bad;
-      if (blockIdx.x == 0) a.held_out[r] = kept;
-    }
-  }
-  const int m = wave_scan(missing), b = wave_scan(wrong);
-  if (lane == 63) {
-    wave[w] = b;
-    miss[w] = m;
-  }
-  __syncthreads();
-  if (blockIdx.x == 0 && tid == 0) {
-    int x = 0, y = 0;
-    for (int k = 0; k < COLLECT_NT / 64; ++k) {
-      x += miss[k];
-      y += wave[k];
-    }
-    a.status[0] = x;
-    a.status[1] = y;
-  }
-  __syncthreads();
-  // free pages below a word: those of the words before
-  const auto free_of = [&](int i) {
-    const int left = n_pages - 32 * i;
-    return ~used[i] & (left >= 32 ? ~0u : (1u << left) - 1);
-  };
-  const int share = (words + gridDim.x - 1) / gridDim.x, lo = blockIdx.x * share < words ? blockIdx.x * share : words,
-            hi = lo + share < words ? lo + share : words;
-  int below = 0, all = 0;
-  for (int i = tid; i < words; i += COLLECT_NT) {
-    const int c = __popc(free_of(i));
-    all += c;
-    if (i < lo) below += c;
-  }
-  below = wave_scan(below);
-  all = wave_scan(all);
-  if (lane == 63) {
-    wave[w] = below;
-    miss[w] = all;
-  }
-  __syncthreads();
-  int start = 0, total = 0;
-  for (int k = 0; k < COLLECT_NT / 64; ++k) {
-    start += wave[k];
-    total += miss[k];
-  }
-  if (blockIdx.x == 0 && tid == 0) a.n_free_out[0] = total;
-  // this share, 1024 words at a time
-  for (int i0 = lo; i0 < hi; i0 += COLLECT_NT) {
-    const int i = i0 + tid;
-    uint32_t f = i < hi ? free_of(i) : 0;
-    const int c = __popc(f), incl = wave_scan(c);
     __syncthreads();
-    if (lane == 63) wave[w] = incl;
-    __syncthreads();
-    int at = start + incl - c;
-    for (int k = 0; k < COLLECT_NT / 64; ++k) {
-      if (k < w) at += wave[k];
-      start += wave[k];
+    // (no lane is masked: entries that count for nothing are read, inside their row, and marked past the pages)
+    const auto mark = [&](int v, bool in) {
+      const unsigned p = (unsigned)v - (unsigned)seg;
+      used[in && p < (unsigned)pages ? p : SEGMENT] = 1;
+      if (last && seg == 0) missing += in && (unsigned)v >= (unsigned)n_pages;
+    };
+    const int64_t step = WAVES * a.d.table_stride;
+    const int32_t* row = a.table + w * a.d.table_stride;
+    const int end = a.d.max_pages - 1;  // (>= 0 where anything is kept)
+    for (int base = 0; base < mine; base += 64, row += 64 * step) {
+      if (base > 0) kept = lengths(base);
+      const uint64_t any = __ballot(kept > 0);
+      // the first 64 entries of 8 rows at once
+#pragma unroll 1
+      for (int g = 0; g < 64 && any >> g; g += 8) {
+        int v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = row[(any >> (g + u) & 1 ? (g + u) * step : 0) + (lane < end ? lane : end)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) mark(v[u], lane < __builtin_amdgcn_readlane(kept, g + u));
+      }
+      // then what longer rows have, 512 at once
+      for (uint64_t more = __ballot(kept > 64); more; more &= more - 1) {
+        const int i = __ffsll((unsigned long long)more) - 1, n = __builtin_amdgcn_readlane(kept, i);
+        const int32_t* at = row + i * step;
+#pragma unroll 1
+        for (int j = 64 + lane; j - lane < n; j += 512) {
+          int v[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u] = at[j + 64 * u < end ? j + 64 * u : end];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) mark(v[u], j + 64 * u < n);
+        }
+      }
     }
-    while (f) {
-      a.free_list[at++] = 32 * i + __ffs(f) - 1;
-      f &= f - 1;
+    __syncthreads();
+    // free pages of this segment below the share, and all of them
+    int below = 0, all = 0;
+    for (int i = tid; i < groups; i += COLLECT_NT) {
+      const u32x4v x = *reinterpret_cast<const u32x4v*>(used + 16 * i);
+      const int c = 16 - (__popc(x[0]) + __popc(x[1]) + __popc(x[2]) + __popc(x[3]));
+      all += c;
+      if (seg + 16 * i < lo) below += c;
+    }
+    at += block_sum(below, tmp);
+    if (last) total += block_sum(all, tmp);
+    // the share's pages of this segment, 16 of them a thread
+    const int g1 = hi - seg < pages ? (hi - seg + 15) >> 4 : groups;
+    for (int g0 = lo > seg ? (lo - seg) >> 4 : 0; g0 < g1; g0 += COLLECT_NT) {
+      const int g = g0 + tid;
+      u32x4v x = {~0u, ~0u, ~0u, ~0u};
+      int c = 0;
+      if (g < g1) {
+        x = *reinterpret_cast<const u32x4v*>(used + 16 * g);
+        c = 16 - (__popc(x[0]) + __popc(x[1]) + __popc(x[2]) + __popc(x[3]));
+      }
+      const int incl = wave_scan(c);
+      __syncthreads();
+      if (lane == 63) tmp[w] = incl;
+      __syncthreads();
+      const int sums = wave_scan(lane < WAVES ? tmp[lane] : 0);
+      int to = at + incl - c + (w > 0 ? __builtin_amdgcn_readlane(sums, w > 0 ? w - 1 : 0) : 0);
+      at += __builtin_amdgcn_readlane(sums, WAVES - 1);
+      int page = seg + 16 * g;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll 1
+        for (uint32_t f = ~x[k] & 0x01010101u; f; f &= f - 1) a.free_list[to++] = page + 4 * k + (__ffs(f) >> 3);
+    }
+    __syncthreads();
+  }
+  if (last) {
+    const int m = block_sum(missing, tmp), b = block_sum(wrong, tmp);
+    if (tid == 0) {
+      a.n_free_out[0] = total;
+      a.status[0] = m;
+      a.status[1] = b;
     }
   }
 }
 
 // ---------------------------------------------------------------------------------
-// Compact.  A workgroup owns one head of K or V of a request.  A row moves down or stays (the kept rows ascend), so what a
-// group of rows overwrites has been read by then: by an earlier group, or by this one, whose loads end before its stores.
+// Compact.  A workgroup owns one head of K or V of a request.  Row i's new place lies below what it holds (others are left
+// out), so a group of rows overwrites nothing that a later one reads, and its own loads end before its stores.
+// Bound by memory where lists are long (a group of 256 rows of 256 bytes, 64 KB, is on its way while the one before is stored;
+// the rows' places are looked up 1024 at a time), by the chain lengths -> numbers -> table -> row where they are short.  4 x 1576
+// of 3152 rows, 40 heads: 69 us for 258 MB (3.7 TB/s); 128 rows at a time, looked up as they are moved, 166.  16 paths of 2 to 6
+// rows, 8 heads 4.0.
 // ---------------------------------------------------------------------------------
-constexpr int MOVE_NT = 256, MOVE_PER = 8;
+constexpr int MOVE_NT = 256, MOVE_PER = 16, MOVE_ROWS = 1024;
 
 template <int CPR>  // 16-byte chunks of a row
 __global__ __launch_bounds__(MOVE_NT) void cache_compact_kernel(const CacheCompactArgs a) {
-  constexpr int RPP = MOVE_NT / CPR;  // rows at once
+  constexpr int RPP = MOVE_NT / CPR, GROUP = RPP * MOVE_PER;  // rows at once
+  __shared__ int64_t from[MOVE_ROWS], to[MOVE_ROWS];  // byte offsets, -1: the row does not move
   const int rv = fdiv(a.by_heads, blockIdx.x), head = blockIdx.x - rv * (int)a.by_heads.d, r = rv >> 1;
   const bool is_v = rv & 1;
   const int q0 = a.q_start[r], q1 = a.q_start[r + 1], n_in = a.q_len ? a.q_len[r] : 0, keep_in = a.n_keep[r], kv = a.kv_len[r];
   const int end = clampi(q1, 0, a.T), room = q0 < 0 || q0 >= end ? 0 : end - q0, n = a.q_len ? clampi(n_in, 0, room) : room;
   const int m = clampi(keep_in, 0, n);
   const int64_t hist = (int64_t)kv - n, width = (int64_t)a.max_pages * a.c.page_size;
-  const int EB = a.c.k_exp ? 1 : 2, ch = threadIdx.x % CPR;
+  const int EB = a.c.k_exp ? 1 : 2, ch = threadIdx.x % CPR, sub = threadIdx.x / CPR;
   char* base = static_cast<char*>(is_v ? a.c.v : a.c.k);
   char* ex = is_v ? nullptr : static_cast<char*>(a.c.k_exp);
   const int32_t* row = a.table + r * a.table_stride;
-  // byte offset of a position's row, -1 where there is none
-  const auto place = [&](int64_t p) -> int64_t {
-    if (p < 0 || p >= width) return -1;
-    const int e = fdiv(a.ps, (int)p), pg = row[e];
+  // the page entry of a position (-1 where there is none), and its row's byte offset
+  const auto page = [&](int64_t p) { return p < 0 || p >= width ? -1 : row[fdiv(a.ps, (int)p)]; };
+  const auto place = [&](int64_t p, int pg) -> int64_t {
     if ((unsigned)pg >= (unsigned)a.c.n_pages) return -1;
-    return ((int64_t)pg * a.c.page_stride + ((int)p - e * a.c.page_size) * a.c.tok_stride + head * a.c.head_stride) * EB;
+    const int in = (int)p - fdiv(a.ps, (int)p) * a.c.page_size;
+    return ((int64_t)pg * a.c.page_stride + in * a.c.tok_stride + head * a.c.head_stride) * EB;
   };
-  for (int i0 = 0; i0 < m; i0 += RPP * MOVE_PER) {
-    u32x4v x[MOVE_PER];
-    uint32_t e4[MOVE_PER];
-    int64_t to[MOVE_PER];
-#pragma unroll
-    for (int u = 0; u < MOVE_PER; ++u) {
-      const int i = i0 + u * RPP + threadIdx.x / CPR;
-      to[u] = -1;
-      if (i >= m) continue;
-      const int k = a.keep[q0 + i];
-      if ((unsigned)k >= (unsigned)n || k == i) continue;
-      const int64_t from = place(hist + k);
-      to[u] = from < 0 ? -1 : place(hist + i);
-      if (to[u] < 0) continue;
-      x[u] = *reinterpret_cast<const u32x4v*>(base + from + 16 * ch);
-      if (ex && ch == 0) e4[u] = *reinterpret_cast<const uint32_t*>(ex + from / 32);
+  for (int s0 = 0; s0 < m; s0 += MOVE_ROWS) {
+    const int rows = m - s0 < MOVE_ROWS ? m - s0 : MOVE_ROWS;
+    for (int i = threadIdx.x; i < rows; i += MOVE_NT) {
+      const int k = a.keep[q0 + s0 + i];
+      const int pt = page(hist + s0 + i);
+      const bool moves = k > s0 + i && k < n;
+      const int pf = moves ? page(hist + k) : -1;
+      const int64_t x = moves ? place(hist + k, pf) : -1, y = moves ? place(hist + s0 + i, pt) : -1;
+      from[i] = x < 0 || y < 0 ? -1 : x;
+      to[i] = y;
     }
     __syncthreads();
+    u32x4v x[MOVE_PER];
+    uint32_t e4[MOVE_PER];
+    const auto load = [&](int i0) {
 #pragma unroll
-    for (int u = 0; u < MOVE_PER; ++u) {
-      if (to[u] < 0) continue;
-      *reinterpret_cast<u32x4v*>(base + to[u] + 16 * ch) = x[u];
-      if (ex && ch == 0) *reinterpret_cast<uint32_t*>(ex + to[u] / 32) = e4[u];
+      for (int u = 0; u < MOVE_PER; ++u) {
+        const int i = i0 + u * RPP + sub;
+        if (i >= rows || from[i] < 0) continue;
+        x[u] = *reinterpret_cast<const u32x4v*>(base + from[i] + 16 * ch);
+        if (ex && ch == 0) e4[u] = *reinterpret_cast<const uint32_t*>(ex + from[i] / 32);
+      }
+    };
+    load(0);
+    for (int i0 = 0; i0 < rows; i0 += GROUP) {
+      // every thread's rows have arrived before any is overwritten
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      u32x4v y[MOVE_PER];
+      uint32_t f4[MOVE_PER];
+#pragma unroll
+      for (int u = 0; u < MOVE_PER; ++u) {
+        y[u] = x[u];
+        f4[u] = e4[u];
+      }
+      if (i0 + GROUP < rows) load(i0 + GROUP);  // (later rows: nothing that is stored now)
+#pragma unroll
+      for (int u = 0; u < MOVE_PER; ++u) {
+        const int i = i0 + u * RPP + sub;
+        if (i >= rows || from[i] < 0) continue;
+        *reinterpret_cast<u32x4v*>(base + to[i] + 16 * ch) = y[u];
+        if (ex && ch == 0) *reinterpret_cast<uint32_t*>(ex + to[i] / 32) = f4[u];
+      }
     }
-    __syncthreads();  // (also for lists that do not ascend: the same result every time)
+    __syncthreads();  // (the places are looked up anew)
   }
 }
 
@@ -341,12 +416,11 @@ hipError_t launch_page_copy(const PageCopyArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_page_collect(const PageCollectArgs& a, hipStream_t s) {
-  const int words = (a.d.n_pages + 31) / 32, groups = words < 64 ? 1 : (words / 64 < 64 ? words / 64 : 64);
-  const dim3 grid((unsigned)groups), block(COLLECT_NT);
-  static_assert(WAM_COLLECT_MAX_PAGES <= 32 * 32768, "bits of the map");
-  if (words <= 1024) hipLaunchKernelGGL(page_collect_kernel<1024>, grid, block, 0, s, a);
-  else if (words <= 8192) hipLaunchKernelGGL(page_collect_kernel<8192>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(page_collect_kernel<32768>, grid, block, 0, s, a);
+  // shares of 4096 pages (16 bytes of marks for a quarter of the threads), more of a pool that 64 workgroups do not cover so
+  const int n = a.d.n_pages, share = n <= 64 * 4096 ? 4096 : ((n + 63) / 64 + 15) / 16 * 16;
+  const dim3 grid((unsigned)(n <= share ? 1 : (n + share - 1) / share)), block(COLLECT_NT);
+  if (n <= COLLECT_SMALL) hipLaunchKernelGGL(page_collect_kernel<COLLECT_SMALL>, grid, block, 0, s, a, share);
+  else hipLaunchKernelGGL(page_collect_kernel<COLLECT_LARGE>, grid, block, 0, s, a, share);
   return hipGetLastError();
 }
 

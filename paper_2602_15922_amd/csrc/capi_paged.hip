@@ -550,6 +550,7 @@ wam_status wam_verify_tree(const wam_verify_tree_desc* desc, const float* p, con
   a.by_slices = fast_div((uint32_t)a.slices);
   a.state = static_cast<VerifyState*>(ws);
   a.sums = reinterpret_cast<double*>(a.state + (int64_t)a.rounds * d.R);
+  a.nodes = reinterpret_cast<float2*>(a.sums + (int64_t)a.rounds * d.R * a.slices);
   HIPCHECK(launch_verify_tree(a, stream));
   return WAM_OK;
 }

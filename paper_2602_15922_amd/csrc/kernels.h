@@ -369,9 +369,9 @@ struct CacheCompactArgs {
 };
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t s);
 
-// Verification of drafted trees: nodes of a request that are looked at, vocabulary entries of a workgroup, passes over the
-// vocabulary by all workgroups (a further one is done by a request's last workgroup alone).
-constexpr int VERIFY_SLICE = 4096, VERIFY_ROUNDS = 2;
+// Verification of drafted trees: vocabulary entries of a workgroup, and the passes over the vocabulary that all of a request's
+// workgroups make, a launch each (further ones are made by its last workgroup alone).
+constexpr int VERIFY_SLICE = 4096, VERIFY_MAX_ROUNDS = 4;
 struct VerifyState {
   double c, s;
   int32_t cur, count, next, done, round, pad[3];
@@ -383,13 +383,20 @@ struct VerifyArgs {
   int32_t *path, *n_path, *next_token, *cache_len;
   VerifyState* state;  // [rounds][R]
   double* sums;        // [rounds][R][slices]
+  float2* nodes;       // [T], drawn: p and q of each node's token at its parent
   int32_t slices, rounds;
   FastDiv by_slices;
 };
-inline int verify_rounds(const wam_verify_tree_desc& d) { return d.drawn ? VERIFY_ROUNDS : 1; }
+// A pass for the last draw and one for each rejection that another child follows: chosen drafts and single ones need one in all;
+// of larger trees the more the more nodes they have.  48 trees of 8 to 32 nodes (17 on average; 1 to 4 passes), V = 100000: 2, 3, 4
+// rounds 51, 44, 36 us; a pass of the last workgroup takes 13 us, one more launch that nobody needs 3.5.
+inline int verify_rounds(const wam_verify_tree_desc& d) {
+  if (!d.drawn || d.T <= 2 * (int64_t)d.R) return 1;
+  return d.T <= 6 * (int64_t)d.R ? 2 : d.T <= 12 * (int64_t)d.R ? 3 : VERIFY_MAX_ROUNDS;
+}
 inline int verify_slices(const wam_verify_tree_desc& d) { return (d.V + VERIFY_SLICE - 1) / VERIFY_SLICE; }
 inline size_t verify_ws_bytes(const wam_verify_tree_desc& d) {
-  return (size_t)verify_rounds(d) * d.R * (sizeof(VerifyState) + 8 * (size_t)verify_slices(d));
+  return (size_t)verify_rounds(d) * d.R * (sizeof(VerifyState) + 8 * (size_t)verify_slices(d)) + (d.drawn ? 8 * (size_t)d.T : 0);
 }
 hipError_t launch_verify_tree(const VerifyArgs& a, hipStream_t s);
 

@@ -44,16 +44,27 @@ struct Nodes {
   int parent[MAX_NODES], token[MAX_NODES];
   float u[MAX_NODES], p[MAX_NODES], q[MAX_NODES];
 };
-template <bool DRAWN, int NT>
-WAM_DEV void load_nodes(const VerifyArgs& a, const Tree& t, Nodes& x) {
+// Their probabilities come from the rows, from the workspace, where the first launch kept them (one trip to memory less), or
+// are not needed (the walk has ended).
+enum Chances { ROWS, KEPT, NONE };
+template <bool DRAWN, int NT, int FROM>
+WAM_DEV void load_nodes(const VerifyArgs& a, const Tree& t, Nodes& x, float2* keep) {
   for (int i = threadIdx.x; i < t.n; i += NT) {
     const int par = a.parent[t.q0 + i], tok = a.tokens[t.q0 + i];
+    const float u = a.u[t.q0 + i];
+    float2 pq = {0.f, 0.f};
+    if (FROM == KEPT) pq = a.nodes[t.q0 + i];
     const bool ok = i > 0 && (unsigned)par < (unsigned)i && (unsigned)tok < (unsigned)a.d.V;
+    if (FROM == ROWS && ok) {
+      pq.x = a.p[(int64_t)(t.q0 + par) * a.d.p_stride + tok];
+      if (DRAWN) pq.y = a.q[(int64_t)(t.q0 + par) * a.d.q_stride + tok];
+    }
     x.parent[i] = ok ? par : -1;
     x.token[i] = tok;
-    x.u[i] = a.u[t.q0 + i];
-    x.p[i] = ok ? a.p[(int64_t)(t.q0 + par) * a.d.p_stride + tok] : 0.f;
-    if (DRAWN) x.q[i] = ok ? a.q[(int64_t)(t.q0 + par) * a.d.q_stride + tok] : 0.f;
+    x.u[i] = u;
+    x.p[i] = pq.x;
+    if (DRAWN) x.q[i] = pq.y;
+    if (keep) keep[t.q0 + i] = pq;
   }
 }
 
@@ -138,24 +149,25 @@ WAM_DEV f32x4 load4(const float* row, int v, int V) {
   return y;
 }
 
-// What is left of 4 entries from v on.  gone: a bit for each entry of the slice, set where its token was rejected (NULL: none).
+// What is left of 4 entries with probabilities p and q.  gone: a bit for each entry of the slice, set where its token was
+// rejected (NULL: none); at: the first one's place in the slice.
 template <bool DRAWN>
-WAM_DEV void left4(const VerifyArgs& a, int64_t row, int v, double c, const uint32_t* gone, int v0, double* y) {
-  const f32x4 p = load4(a.p + row * a.d.p_stride, v, a.d.V);
-  if (DRAWN && c != 0.0) {
-    const f32x4 q = load4(a.q + row * a.d.q_stride, v, a.d.V);
+WAM_DEV void left4(f32x4 p, f32x4 q, double c, const uint32_t* gone, int at, double* y) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = left_of(p[e], q[e], c);
-  } else {
+  for (int e = 0; e < 4; ++e) y[e] = DRAWN ? left_of(p[e], q[e], c) : left_of(p[e]);
+  if (!DRAWN && gone) {
+    const uint32_t bits = gone[at >> 5] >> (at & 31);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = left_of(p[e]);
-    if (!DRAWN && gone) {
-      const uint32_t bits = gone[(v - v0) >> 5] >> ((v - v0) & 31);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (bits >> e & 1) y[e] = 0.0;
-    }
+    for (int e = 0; e < 4; ++e)
+      if (bits >> e & 1) y[e] = 0.0;
   }
+}
+// 4 entries of p and q (0 where nothing of it is taken away) at node row from v on
+template <bool DRAWN>
+WAM_DEV void load_pq(const VerifyArgs& a, int64_t row, int v, bool taken, f32x4& p, f32x4& q) {
+  p = load4(a.p + row * a.d.p_stride, v, a.d.V);
+  q = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (DRAWN && taken) q = load4(a.q + row * a.d.q_stride, v, a.d.V);
 }
 
 // marks the slice's tokens that were rejected at node st.cur (every thread of the workgroup, barriers inside)
@@ -179,44 +191,55 @@ WAM_DEV double join(const double* sums, int slices) {
   return wave_sum_f64(s);
 }
 
-// One workgroup per request and slice: walks to the next sum, and sums its slice.
-constexpr int SUM_NT = 256;
-template <bool DRAWN>
+// One workgroup per request and slice: walks to the next sum, and sums its slice.  In a later round the rows of the node
+// where the last one stopped are on their way while it walks (it stops there again where the next child is rejected too).
+constexpr int SUM_NT = 256, SUM_PER = SLICE / (4 * SUM_NT);
+template <bool DRAWN, bool LATER>
 __global__ __launch_bounds__(SUM_NT) void verify_sum_kernel(const VerifyArgs a, int round) {
   __shared__ Nodes x;
   __shared__ uint32_t gone[SLICE / 32];
   __shared__ double part[SUM_NT / 64];
   const int r = fdiv(a.by_slices, blockIdx.x), slice = blockIdx.x - r * a.slices, tid = threadIdx.x, w = tid >> 6;
+  const int v0 = slice * SLICE;
+  VerifyState st = first_state();
+  double s = 1.0;
+  if (LATER) {
+    st = a.state[(int64_t)(round - 1) * a.d.R + r];
+    s = join(a.sums + ((int64_t)(round - 1) * a.d.R + r) * a.slices, a.slices);
+  }
   const Tree t = tree_of(a, r);
   if (t.n == 0) return;
-  VerifyState st = first_state();
-  if (round > 0) {
-    st = a.state[(int64_t)(round - 1) * a.d.R + r];
-    if (st.done) {
-      if (slice == 0 && tid == 0) a.state[(int64_t)round * a.d.R + r] = st;
-      return;
-    }
-    st.s = join(a.sums + ((int64_t)(round - 1) * a.d.R + r) * a.slices, a.slices);
+  if (LATER && st.done) {
+    if (slice == 0 && tid == 0) a.state[(int64_t)round * a.d.R + r] = st;
+    return;
   }
-  load_nodes<DRAWN, SUM_NT>(a, t, x);
+  st.s = s;
+  f32x4 p[SUM_PER], q[SUM_PER];
+  const auto load = [&] {
+#pragma unroll
+    for (int k = 0; k < SUM_PER; ++k) load_pq<DRAWN>(a, t.q0 + st.cur, v0 + 4 * (k * SUM_NT + tid), st.c != 0.0, p[k], q[k]);
+  };
+  const int was = st.cur;
+  if (LATER) load();  // (c > 0: it stopped at a rejection)
+  load_nodes<DRAWN, SUM_NT, LATER ? KEPT : ROWS>(a, t, x, DRAWN && !LATER && slice == 0 ? a.nodes : nullptr);
   __syncthreads();
   int32_t* path = slice == 0 && w == 0 ? a.path + t.q0 : nullptr;
-  if (path && round == 0 && tid == 0) path[0] = 0;
+  if (path && !LATER && tid == 0) path[0] = 0;
   walk<DRAWN>(x, t.n, st, path);
   st.round = round;
   if (slice == 0 && tid == 0) a.state[(int64_t)round * a.d.R + r] = st;
-  const int v0 = slice * SLICE;
+  if (!LATER || st.cur != was) load();
   const bool some = !DRAWN && st.next > 1;
   if (some) mark_gone<SUM_NT>(x, t.n, st, v0, gone);
-  double s = 0.0;
+  double sum = 0.0;
 #pragma unroll
-  for (int k = 0; k < SLICE / (4 * SUM_NT); ++k) {
+  for (int k = 0; k < SUM_PER; ++k) {
     double y[4];
-    left4<DRAWN>(a, t.q0 + st.cur, v0 + 4 * (k * SUM_NT + tid), st.c, some ? gone : nullptr, v0, y);
-    s += (y[0] + y[1]) + (y[2] + y[3]);
+    left4<DRAWN>(p[k], q[k], st.c, some ? gone : nullptr, 4 * (k * SUM_NT + tid), y);
+    sum += (y[0] + y[1]) + (y[2] + y[3]);
   }
-  s = wave_sum_f64(s);
-  if ((tid & 63) == 0) part[w] = s;
+  sum = wave_sum_f64(sum);
+  if ((tid & 63) == 0) part[w] = sum;
   __syncthreads();
   if (tid == 0) a.sums[((int64_t)round * a.d.R + r) * a.slices + slice] = (part[0] + part[1]) + (part[2] + part[3]);
 }
@@ -231,6 +254,8 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
   __shared__ int found, last_of[END_NT / 64];
   static_assert(SLICE == 4 * END_NT, "a slice is four entries per thread");
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  VerifyState st = a.state[(int64_t)(a.rounds - 1) * a.d.R + r];  // (of a request without rows: anything)
+  const float u_next = a.u_next[r];
   const Tree t = tree_of(a, r);
   if (t.n == 0) {
     if (tid == 0) {
@@ -240,53 +265,48 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
     }
     return;
   }
-  const int last_round = a.rounds - 1;
-  VerifyState st = a.state[(int64_t)last_round * a.d.R + r];
-  load_nodes<DRAWN, END_NT>(a, t, x);
-  {
-    const double* sums = a.sums + ((int64_t)st.round * a.d.R + r) * a.slices;
-    for (int i = tid; i < a.slices; i += END_NT) own[i] = sums[i];
-  }
-  __syncthreads();
-  // sum of a slice by the workgroup (barriers inside; the same in every thread)
-  const auto slice_sum = [&](int slice, bool whole_p) {
-    double y[4];
-    left4<DRAWN>(a, t.q0 + st.cur, slice * SLICE + 4 * tid, whole_p ? 0.0 : st.c, nullptr, slice * SLICE, y);
-    const double s = wave_sum_f64((y[0] + y[1]) + (y[2] + y[3]));
-    __syncthreads();
-    if (lane == 0) part[w] = s;
-    __syncthreads();
-    double all = 0.0;
-    for (int k = 0; k < END_NT / 64; ++k) all += part[k];
-    return all;
-  };
+  const double* sums = a.sums + ((int64_t)st.round * a.d.R + r) * a.slices;
+  if (!DRAWN) load_nodes<DRAWN, END_NT, NONE>(a, t, x, nullptr);
+  else if (!st.done) load_nodes<DRAWN, END_NT, KEPT>(a, t, x, nullptr);
+  // the sums of all slices, a wavefront for each
   const auto sum_all = [&](bool whole_p) {
-    for (int i = 0; i < a.slices; ++i) {
-      const double s = slice_sum(i, whole_p);
-      if (tid == 0) own[i] = s;
+    for (int i = w; i < a.slices; i += END_NT / 64) {
+      double s = 0.0;
+#pragma unroll 8
+      for (int k = 0; k < SLICE / 256; ++k) {
+        double y[4];
+        f32x4 p, q;
+        load_pq<DRAWN>(a, t.q0 + st.cur, i * SLICE + 256 * k + 4 * lane, !whole_p && st.c != 0.0, p, q);
+        left4<DRAWN>(p, q, st.c, nullptr, 0, y);
+        s += (y[0] + y[1]) + (y[2] + y[3]);
+      }
+      s = wave_sum_f64(s);
+      if (lane == 0) own[i] = s;
     }
     __syncthreads();
+    sums = own;
   };
+  __syncthreads();
   while (!st.done) {
-    st.s = join(own, a.slices);
+    st.s = join(sums, a.slices);
     walk<DRAWN>(x, t.n, st, w == 0 ? a.path + t.q0 : nullptr);
     __syncthreads();  // (everybody has joined)
     sum_all(false);
   }
-  double total = join(own, a.slices);
+  double total = join(sums, a.slices);
   bool whole_p = false;  // nothing is left: the token is drawn from the target's probabilities themselves
   if (!(total > 0.0)) {
     whole_p = true;
     __syncthreads();
     sum_all(true);
-    total = join(own, a.slices);
+    total = join(sums, a.slices);
   }
   // the first slice whose sum up to its end exceeds the threshold, or the last with any; by the first wavefront's lanes
-  const double goal = (double)a.u_next[r] * total;
+  const double goal = (double)u_next * total;
   int slice = -1, some = -1;
   double before = 0.0, at = 0.0;
   for (int b = 0; b < a.slices && slice < 0; b += 64) {
-    const double s = b + lane < a.slices ? own[b + lane] : 0.0, incl = wave_scan_f64(s) + before;
+    const double s = b + lane < a.slices ? sums[b + lane] : 0.0, incl = wave_scan_f64(s) + before;
     const uint64_t over = __ballot(incl > goal && s > 0.0), any = __ballot(s > 0.0);
     const int hit = over ? __ffsll((unsigned long long)over) - 1 : (any ? 63 - __clzll((long long)any) : -1);
     if (hit >= 0) {
@@ -302,7 +322,9 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
     const bool marked = !DRAWN && !whole_p && st.next > 1;
     if (marked) mark_gone<END_NT>(x, t.n, st, v0, gone);
     double y[4];
-    left4<DRAWN>(a, t.q0 + st.cur, v0 + 4 * tid, whole_p ? 0.0 : st.c, marked ? gone : nullptr, v0, y);
+    f32x4 p, q;
+    load_pq<DRAWN>(a, t.q0 + st.cur, v0 + 4 * tid, !whole_p && st.c != 0.0, p, q);
+    left4<DRAWN>(p, q, st.c, marked ? gone : nullptr, 4 * tid, y);
     const double mine = (y[0] + y[1]) + (y[2] + y[3]), incl = wave_scan_f64(mine);
     if (tid == 0) found = INT32_MAX;
     if (lane == 63) part[w] = incl;
@@ -341,8 +363,10 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
 
 template <bool DRAWN>
 hipError_t launch(const VerifyArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.d.R * a.slices)), block(SUM_NT);
   for (int i = 0; i < a.rounds; ++i) {
-    hipLaunchKernelGGL(verify_sum_kernel<DRAWN>, dim3((unsigned)((int64_t)a.d.R * a.slices)), dim3(SUM_NT), 0, s, a, i);
+    if (i == 0) hipLaunchKernelGGL((verify_sum_kernel<DRAWN, false>), grid, block, 0, s, a, i);
+    else if (DRAWN) hipLaunchKernelGGL((verify_sum_kernel<true, true>), grid, block, 0, s, a, i);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

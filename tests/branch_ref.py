@@ -76,13 +76,13 @@ def place(table, n_pages, ps, r, p):
 
 
 def compact(x, table, q_start, q_len, kv_len, keep, n_keep, ps):
-    """x [n_pages, ps, ...] after the call: all rows read before any is written (for numbers that ascend)."""
+    """x [n_pages, ps, ...] after the call: all rows read before any is written."""
     y = x.clone()
     for r, (at, n) in enumerate(rows_of(q_start, q_len, len(keep))):
         hist = int(kv_len[r]) - n
         for i in range(min(max(int(n_keep[r]), 0), n)):
             k = int(keep[at + i])
-            if 0 <= k < n and k != i:
+            if i < k < n:
                 a, b = place(table, len(x), ps, r, hist + k), place(table, len(x), ps, r, hist + i)
                 if a and b:
                     y[b] = x[a]

@@ -166,7 +166,8 @@ def run_collect(cache_len, held, table, n_pages, ps, gap=3):
 
 @pytest.mark.parametrize("R,width,ps,n_pages", [
     (0, 4, 16, 50), (1, 1, 16, 1), (3, 5, 64, 20), (3, 5, 64, 0), (7, 40, 16, 31), (7, 40, 16, 32), (7, 40, 16, 33), (50, 300, 48, 9000), (16, 64, 16, 32767),
-    (16, 64, 16, 32769), (1030, 20, 16, 40000), (4096, 3, 32, 20000), (5, 2000, 16, 300001), (3, 4, 16, 1 << 20)])
+    (16, 64, 16, 32769), (1030, 20, 16, 40000), (4096, 3, 32, 20000), (5, 2000, 16, 155648), (90, 2000, 16, 155649), (5, 2000, 16, 300001),
+    (3, 4, 16, 1 << 20), (40, 3001, 16, 700007)])
 def test_collect(R, width, ps, n_pages):
     g = np.random.default_rng(R + width)
     held = g.integers(0, width + 1, R)
@@ -261,18 +262,16 @@ def test_compact_padded_absent_and_out_of_range():
             run_compact(b, np.arange(b.T)[::-1].copy(), [3, 50, 50, 50, 50], q_start=starts, kv_len=kv)
 
 
-def test_compact_gives_the_same_twice_for_any_list():
-    """Numbers that do not ascend: unspecified rows, but the same at every call, and no others than they name."""
-    import torch
-    g = np.random.default_rng(9)
-    keep = g.integers(0, 700, 703)
-    out = []
-    for _ in range(2):
-        b = Batch([(700, 800)], 2, 2, 128, 16, seed=7, junk=1.0)
-        log("compact any list")
-        run_compact(b, keep, [700])
-        out.append((b.dk.cpu(), b.dv.cpu()))
-    assert all(torch.equal(x, y) for x, y in zip(*out))
+@pytest.mark.parametrize("n", [9, 700, 3000])
+def test_compact_of_any_list(n):
+    """Numbers in any order, again and again the same, out of range: those past their place move, as all rows were before."""
+    g = np.random.default_rng(n)
+    b = Batch([(n, n + 100)], 2, 2, 128, 16, seed=7, junk=1.0)
+    keep = g.integers(-5, n + 5, b.T)
+    log(f"compact any list {n}")
+    check_compact(b, keep, [n])
+    keep[:] = n - 1
+    check_compact(b, keep, [n])
 
 
 def test_offsets_past_32_bits():
