@@ -149,7 +149,7 @@ wam_status run_paged(const wam_attn_paged_desc& d, const wam_paged_cache& c, con
   TRY(need_ints(kv_len, "kv_len"));
   if (d.max_pages > 0) TRY(need_ints(block_table, "block_table"));
   const RaggedPlan p = plan(d.R, d.T, d.Hq, c.Hkv, c.Dh, d.max_kv);
-  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh)));
+  TRY(check_ws(ws, ws_bytes, ragged_ws_bytes(p, d.T, d.Hq, c.Dh, ragged_tiles(d.R, d.T, d.Hq, c.Hkv, p.rows))));
   TRY(check_launch(ragged_blocks(p, d.R, d.T, d.Hq, c.Hkv) * 256 * p.groups));
   a.q = q; a.k = c.k; a.v = c.v; a.k_exp = c.k_exp; a.o = o;
   // (a table without columns is never read: no key is below max_k = 0; its address only says "paged")
@@ -474,7 +474,8 @@ wam_status wam_cache_compact(const wam_cache_compact_desc* desc, const wam_paged
 
 size_t wam_attn_tree_workspace_bytes(const wam_attn_tree_desc* desc, const wam_paged_cache* cache) {
   if (!desc || !cache || check_ragged(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv) != WAM_OK) return 0;
-  return ragged_ws_bytes(plan_tree(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv), desc->T, desc->Hq, cache->Dh);
+  const RaggedPlan p = plan_tree(desc->R, desc->T, desc->Hq, cache->Hkv, cache->Dh, desc->max_kv);
+  return ragged_ws_bytes(p, desc->T, desc->Hq, cache->Dh, ragged_tiles(desc->R, desc->T, desc->Hq, cache->Hkv, p.rows));
 }
 
 wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* cache, const void* q,

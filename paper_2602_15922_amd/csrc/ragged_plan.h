@@ -14,6 +14,7 @@ struct RaggedPlan {
   int groups = 1;          // groups of four wavefronts of a workgroup of the tile kernel
   int splits = 1;          // workgroups along the key axis, at most
   int split_keys = 0;      // keys of each (a multiple of 128)
+  int hull = 0;            // tile kernel of trees with long masks: which new tokens a row tile's rows see is found first
   int turns = 0;           // tile kernel of trees: parts and requests in turn over the XCDs
 };
 
@@ -75,13 +76,16 @@ inline int64_t ragged_tiles(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int r
 inline RaggedPlan plan_tree(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t Dh, int64_t max_k) {
   RaggedPlan p = plan_ragged(R, T, Hq, Hkv, Dh, max_k);
   const int64_t rows = T * (Hq / Hkv);
+  p.hull = p.rows == RAGGED_ROWS && p.groups == 1 && T >= 512 * R;
   if (rows <= 16 * R || rows > 4 * RAGGED_ROWS * R || R <= 1) return p;
   // 17 to 512 rows on average: the tile kernel, which streams requests of up to 32 rows and reads the keys of the others once
   // for 128 rows (48 requests of 5 to 60 rows, E4M3, 1048-32012 keys: 240 us; the streaming kernel with 32 rows 267).  Parts of
   // 2048 keys unless there are thousands of workgroups without, in turn over the XCDs: 16 requests of 96 to 256 rows, 8 heads,
   // 332-16064 keys at 1024, 1536, 2048, 4096 keys 123, 127, 105, 160 us (by row tile and head on the XCDs 234, 225, 224, 202);
   // the 48 requests 264, 259, 240, 257 us.
+  const int hull = p.hull;
   p = RaggedPlan{};
+  p.hull = hull;
   const int64_t per = (rows + p.rows - 1) / p.rows, tiles = (R < T ? R : T) > per ? (R < T ? R : T) : per;
   int64_t n = 8192 / (tiles * Hkv > 0 ? tiles * Hkv : 1);
   const int64_t by_keys = (max_k + 2047) / 2048;
@@ -107,8 +111,11 @@ inline int64_t ragged_blocks(const RaggedPlan& p, int64_t R, int64_t T, int64_t 
 inline size_t ragged_ml_bytes(const RaggedPlan& p, int64_t T, int64_t Hq) {
   return ((size_t)T * Hq * p.splits * 8 + 255) / 256 * 256;
 }
-inline size_t ragged_ws_bytes(const RaggedPlan& p, int64_t T, int64_t Hq, int64_t Dh) {
+inline size_t ragged_parts_bytes(const RaggedPlan& p, int64_t T, int64_t Hq, int64_t Dh) {
   return p.splits <= 1 ? 0 : ragged_ml_bytes(p, T, Hq) + (size_t)T * Hq * p.splits * Dh * 4;
+}
+inline size_t ragged_ws_bytes(const RaggedPlan& p, int64_t T, int64_t Hq, int64_t Dh, int64_t tiles = 0) {
+  return ragged_parts_bytes(p, T, Hq, Dh) + (p.hull ? (size_t)tiles * 8 : 0);
 }
 
 }  // namespace wam

@@ -121,6 +121,53 @@ def test_causal_mask_is_the_causal_attention(lens, Hq, Hkv, Dh):
         assert np.all((np.abs(got - want) <= 2 * paged_ref.attention_tolerance(a))[mine])
 
 
+def bits_of(sees):
+    """Mask rows of a truth table [n][n]."""
+    n = len(sees)
+    out = np.zeros((n, -(-n // 32) * 32), np.uint8)
+    out[:, :n] = sees
+    return np.packbits(out, axis=1, bitorder="little").view(np.int32)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh,fp8", [([(2600, 2700), (40, 300)], 1, 1, 64, False), ([(2500, 2531), (70, 70)], 2, 1, 128, False),
+                                                ([(2300, 2900), (3, 100)], 1, 1, 128, True), ([(1300, 1400), (1290, 1290), (1500, 3000)], 1, 1, 64, False)])
+def test_long_masks(lens, Hq, Hkv, Dh, fp8):
+    """Masks of thousands of tokens, whose rows see nothing of long stretches: before their own branch, behind it, or of all new
+    tokens; with pages missing, and values that are not finite in what is not seen."""
+    from ragged_plans import plan
+    b = Batch(lens, Hq, Hkv, Dh, 16, seed=19, fp8=fp8)
+    assert b.T >= 512 * len(lens) and plan(len(lens), b.T, Hq, Hkv, Dh, b.width * 16)["groups"] == 1
+    i = {n: np.arange(n) for n, _ in lens}
+    kinds = {
+        "branches": lambda n: i[n][:, None] * 2 // n == i[n] * 2 // n, "late": lambda n: (i[n] >= n - 40) & (i[n][:, None] % 3 > 0),
+        "early": lambda n: (i[n] < 5) & (i[n][:, None] < 2000), "none": lambda n: np.zeros((n, n), bool), "self": lambda n: np.eye(n, dtype=bool),
+        "apart": lambda n: (i[n] % 1100 == 7) & (i[n] <= i[n][:, None])}
+    for name, sees in kinds.items():
+        mask = np.zeros((b.T, max(-(-n // 32) for n, _ in lens)), np.int32)
+        for at, (n, _) in zip(b.q_start, lens):
+            rows = bits_of(sees(n))
+            mask[at:at + n, :rows.shape[1]] = rows
+        log(f"tree long masks {lens} Hq={Hq} Dh={Dh} fp8={fp8} {name}")
+        check(run_tree(b, mask), expected(b, mask), name)
+    table = b.table.copy()
+    b.table[0, 20:60] = -1
+    check(run_tree(b, mask), expected(b, mask), "absent")
+    b.table = table
+    n, m = lens[0]
+    for back in (n - 100, 900, 3):
+        j = m - back  # tokens that only some rows see, or none
+        b.v[b.table[0, j // 16], j % 16] = 0x7F if fp8 else float("nan")
+    mask[:] = 0
+    for at, (n, _) in zip(b.q_start, lens):
+        rows = bits_of(kinds["branches"](n))
+        mask[at:at + n, :rows.shape[1]] = rows
+    log(f"tree long masks {lens} not finite")
+    got, (o, a, mine) = run_tree(b, mask), expected(b, mask)
+    assert np.array_equal(np.isnan(got), np.isnan(o) & mine[:, None, None])
+    fin = mine[:, None, None] & np.isfinite(o)
+    assert np.all(np.abs(got[fin] - o[fin]) <= paged_ref.attention_tolerance(a)[fin])
+
+
 def test_words_of_the_mask():
     """Fewer words than tokens (the rest is seen by nobody), more, none; rows apart."""
     b = Batch([(70, 200), (3, 100), (33, 33)], 4, 2, 128, 16, seed=6)

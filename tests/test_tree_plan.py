@@ -15,7 +15,8 @@ ENTRY = """#include "ragged_plan.h"
 extern "C" void tree(long R, long T, long Hq, long Hkv, long Dh, long max_k, long* out) {
   const wam::RaggedPlan p = wam::plan_tree(R, T, Hq, Hkv, Dh, max_k);
   out[0] = p.rows; out[1] = p.groups; out[2] = p.splits; out[3] = p.split_keys; out[4] = p.turns;
-  out[5] = wam::ragged_tiles(R, T, Hq, Hkv, p.rows); out[6] = (long)wam::ragged_ws_bytes(p, T, Hq, Dh);
+  out[5] = wam::ragged_tiles(R, T, Hq, Hkv, p.rows); out[6] = (long)wam::ragged_ws_bytes(p, T, Hq, Dh, wam::ragged_tiles(R, T, Hq, Hkv, p.rows));
+  out[8] = p.hull;
   out[7] = wam::ragged_blocks(p, R, T, Hq, Hkv);
 }
 """
@@ -32,9 +33,9 @@ def _lib():
 
 
 def tree(*args):
-    out = (ctypes.c_long * 8)()
+    out = (ctypes.c_long * 9)()
     _lib().tree(*(ctypes.c_long(x) for x in args), out)
-    return dict(zip(("rows", "groups", "splits", "keys", "turns", "tiles", "ws", "blocks"), out))
+    return dict(zip(("rows", "groups", "splits", "keys", "turns", "tiles", "ws", "blocks", "hull"), out))
 
 
 def test_every_plan_covers_the_keys_and_can_be_joined():
@@ -49,13 +50,15 @@ def test_every_plan_covers_the_keys_and_can_be_joined():
         assert p["keys"] % 128 == 0 and p["keys"] >= 128 and p["keys"] * p["splits"] >= max_k
         assert (p["splits"] - 1) * p["keys"] < max(max_k, 1)
         assert p["groups"] == 1 or (p["rows"] == 128 and R == 1)
-        assert p["ws"] == 0 if p["splits"] == 1 else p["ws"] >= T * Hq * p["splits"] * (Dh * 4 + 8)
+        hull = 8 * p["tiles"] if p["hull"] else 0
+        assert p["ws"] == hull if p["splits"] == 1 else p["ws"] >= T * Hq * p["splits"] * (Dh * 4 + 8) + hull
+        assert not p["hull"] or (p["rows"] == 128 and p["groups"] == 1)
         # every (row tile, part, head) has its workgroup
         assert p["blocks"] >= p["tiles"] * p["splits"] * Hkv and (not p["turns"] or p["blocks"] % (8 * Hkv) == 0)
 
 
 def test_one_request_and_few_rows_are_the_paged_attentions():
-    for args in ((1, 300, 8, 2, 128, 5000), (9, 40, 8, 8, 128, 700), (1, 6304, 40, 40, 128, 12608), (40, 40, 32, 8, 64, 9000)):
+    for args in ((1, 300, 8, 2, 128, 5000), (9, 40, 8, 8, 128, 700), (1, 200, 40, 40, 128, 12608), (40, 40, 32, 8, 64, 9000)):
         p, want = tree(*args), plan(*args)
         assert {k: p[k] for k in want} == want and p["turns"] == 0
 
@@ -63,7 +66,7 @@ def test_one_request_and_few_rows_are_the_paged_attentions():
 @pytest.mark.parametrize("args,want", [
     ((16, 681, 32, 8, 128, 16064), dict(rows=128, splits=8, keys=2048, turns=1)),   # drafted trees, a shared-head decoder
     ((48, 225, 40, 8, 128, 32012), dict(rows=128, splits=16, keys=2048, turns=1)),              # small trees over long histories
-    ((2, 12608, 40, 40, 128, 18912), dict(rows=128, splits=1, turns=0))])           # two robots' video branches
+    ((2, 12608, 40, 40, 128, 18912), dict(rows=128, splits=1, turns=0, hull=1))])           # two robots' video branches
 def test_documented_plans(args, want):
     p = tree(*args)
     assert {k: p[k] for k in want} == want, p
