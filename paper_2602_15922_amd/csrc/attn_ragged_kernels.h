@@ -37,13 +37,19 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // pages, the history and the new tokens whose bit is set in the row's mask.
 enum Keys { STATES = 0, PAGES = 1, TREE = 2 };
 
+// Of the new tokens, those that some row of a row tile sees: from `first` to before `past` (0: none); and those from `first` to
+// before `whole` all of its rows see.
+struct Hull {
+  int first, past, whole;
+};
+
 struct Parts {
   float* ml;  // [row][splits][2]: reference and sum
   float* o;   // [row][splits][Dh]
   int splits, split_keys, tiles;
   int turns;  // tree, tile kernel: parts and requests in turn over the XCDs, as the streaming kernel has them
   FastDiv by_splits, by_tiles, by_heads;
-  const int32_t* hull;  // tree, long masks: [row tile][2], first and one past the last new token that its rows see; or NULL
+  const Hull* hull;  // tree, long masks: of each row tile of the tile kernel, or NULL
 };
 
 WAM_DEV int fdiv(const FastDiv& f, int n) {
@@ -704,7 +710,7 @@ WAM_DEV void tile_arrived() {
 // False, and nothing is written: V of keys that only some of the rows see holds values that are not finite.
 template <int DH, int KEYS, bool FP8, int GROUPS>
 WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
-                       bool whole, int start, int end, int meta, bf16* smem_all, int* odd, int gap, int past) {
+                       bool whole, int start, int end, int meta, bf16* smem_all, int* odd, int gap, int past, int seen, int past_seen) {
   constexpr int KS = DH / 16, MT = DH / 32, TILE = 2 * BN * DH;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int w = uniform(tid >> 6) & 3, grp = GROUPS == 1 ? 0 : uniform(tid >> 8);
@@ -782,13 +788,20 @@ WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
       meta = meta_next;
     }
   }
-  for (int wb = t0; wb < (idle ? t0 : nt); wb = window(wb)) {
+  // tree: the first tile that every row sees among the new tokens' (in the first buffer's turn)
+  const int again = KEYS == TREE && GROUPS == 1 ? seen + ((seen - t0) & 1) : 0;
+  int from = t0;
+  for (int wb = t0; wb < (idle ? t0 : nt);) {
     const int we = wb + 16 < nt ? wb + 16 : nt;
     meta_next = page_of<KEYS>(a, r, window(wb) * BN + 16 * lane);
     // (groups past the end count as present: the rows' prefixes hide them)
     const uint64_t there = __ballot(meta >= 0 || wb * BN + 16 * lane >= end);
-    const int plain = ~there == 0 ? (n_plain < we ? n_plain : we) : wb;
-    int tb = wb;  // the groups' tiles tb .. tb + GROUPS - 1
+    int plain = ~there == 0 ? (n_plain < we ? n_plain : we) : wb, stop = we;
+    if constexpr (KEYS == TREE && GROUPS == 1) {
+      if (from >= again) plain = ~there == 0 ? (past_seen < we ? past_seen : we) : wb;
+      else if (again < we && again < past_seen) stop = again;
+    }
+    int tb = from;  // the groups' tiles tb .. tb + GROUPS - 1
     auto step = [&](int cur, auto mask) {
       const int t = tb + grp;
       if (GROUPS == 1 || t < nt) {
@@ -833,7 +846,13 @@ WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r
       step(0, std::false_type{});
       step(1, std::false_type{});
     }
-    while (tb < we) step((tb - t0) / GROUPS & 1, std::true_type{});
+    while (tb < stop) step((tb - t0) / GROUPS & 1, std::true_type{});
+    if (KEYS == TREE && GROUPS == 1 && tb < we) {  // (the window's second part)
+      from = tb;
+      continue;
+    }
+    wb = window(wb);
+    from = wb;
     meta = meta_next;
   }
 
@@ -946,7 +965,8 @@ WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane)
 struct Work {
   Req q;
   int r, hk, G, m0, split, start, end;
-  int gap, past;  // tree: the tiles gap .. past - 1 are seen by no row (windows of 16 of them)
+  int gap, past;        // tree: the tiles gap .. past - 1 are seen by no row (windows of 16 of them),
+  int seen, past_seen;  // the tiles seen .. past_seen - 1 by every row
   int meta;    // lane: page of a group of the first keys
   bool whole;  // the request has one part: the output itself is written
 };
@@ -991,11 +1011,19 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, int block, Work& k)
   k.end = kmax - k.start < pt.split_keys ? kmax : k.start + pt.split_keys;
   if constexpr (KEYS == TREE && SHIFT == 7) {
     k.gap = k.past = INT32_MAX;
+    k.seen = 1 << 30;  // (none)
+    k.past_seen = 0;
     if (pt.hull) {
-      const int64_t history = (int64_t)k.q.kv - k.q.n, first = history + pt.hull[2 * x], past = history + pt.hull[2 * x + 1];
+      const Hull h = pt.hull[x];
+      const int64_t history = (int64_t)k.q.kv - k.q.n, first = history + h.first, past = history + h.past;
       const int known = history < 0 ? 0 : (int)history;  // (below 2^31)
       const int64_t end = past > known ? past : known;
       if (end < k.end) k.end = (int)end;
+      const int64_t whole = history + h.whole < k.end ? history + h.whole : k.end;
+      if (first >= 0 && whole > first) {
+        k.seen = (int)((first + BN - 1) / BN);
+        k.past_seen = (int)(whole / BN);
+      }
       const int t0 = k.start / BN, from = known / BN + 1, gap = from <= t0 ? t0 : t0 + (from - t0 + 15) / 16 * 16;
       if (first / BN >= gap + 16 && first > 0) {
         k.gap = gap;
@@ -1027,7 +1055,7 @@ __global__ __launch_bounds__(NT * GROUPS, DH == 64 ? 3 : 2) void ragged_tile_ker
   if (!find_work<KEYS, 7>(a, pt, blockIdx.x, k)) return;
   int last = k.m0 + 1;  // streamed: the rows m0 .. last - 1, 32 at a time
   if (GROUPS == 2 || k.q.n * k.G > RAGGED_STREAM) {
-    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem, odd, k.gap, k.past))
+    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem, odd, k.gap, k.past, k.seen, k.past_seen))
       return;
     int block = blockIdx.x;  // (found anew, so that nothing is kept for it: two samples' 3152 rows 1861 -> 1831 us)
     asm volatile("" : "+s"(block) : : "memory");
@@ -1144,10 +1172,13 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
   }
 }
 
-// First and one past the last new token that some row of a row tile of the tile kernel sees (past 0: none).  Before the first and
-// behind the last the tile kernel loads nothing: two futures of 3152 rows over 6304 keys, 40 heads, 1563 -> 1416 us, of which this takes 11.
-__global__ __launch_bounds__(NT) void tree_hull_kernel(const RaggedArgs a, const Parts pt, int32_t* hull) {
-  __shared__ int lo_of[4], hi_of[4];
+// The hulls: before the first token that a row tile's rows see and behind the last the tile kernel loads nothing, and what all
+// of them see it does not mask (two futures of 3152 rows over 6304 keys, 40 heads: 1563 us without, 1416 without the last, 1387; of
+// this 8).  A workgroup per row tile, its tokens in turn over the wavefronts, the masks' words over the lanes.
+constexpr int HULL_NT = 512, HULL_KEPT = 4;
+__global__ __launch_bounds__(HULL_NT) void tree_hull_kernel(const RaggedArgs a, const Parts pt, Hull* hull) {
+  constexpr int WAVES = HULL_NT / 64;
+  __shared__ int of[3][WAVES];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), x = blockIdx.x, G = (int)a.group.d;
   const int r = uniform(find_request(a, x, G, 7, lane));
   if (r < 0) return;
@@ -1155,19 +1186,39 @@ __global__ __launch_bounds__(NT) void tree_hull_kernel(const RaggedArgs a, const
   const int64_t m0 = ((int64_t)x - r - (((int64_t)q.q0 * G) >> 7)) * RAGGED_ROWS;
   const int rows = q.n * G;
   if (m0 < 0 || m0 >= rows) return;
-  const int first = fdiv(a.group, (int)m0), last = fdiv(a.group, m0 + RAGGED_ROWS <= rows ? (int)m0 + RAGGED_ROWS - 1 : rows - 1);
-  const int all = (q.n - 1) / 32 + 1, words = a.mask_words < all ? a.mask_words : all;
+  const int begin = fdiv(a.group, (int)m0), last = fdiv(a.group, m0 + RAGGED_ROWS <= rows ? (int)m0 + RAGGED_ROWS - 1 : rows - 1);
+  const int every = (q.n - 1) / 32 + 1, words = a.mask_words < every ? a.mask_words : every;
   int lo = INT32_MAX, hi = 0;
-  for (int c = lane; c < words; c += 64) {
+  uint32_t kept[HULL_KEPT];  // the tokens that all of the wavefront's see, of the first 64 * HULL_KEPT words
+  const auto scan = [&](int c, uint32_t& all) {
     uint32_t any = 0;
-#pragma unroll 8
-    for (int tok = first + w; tok <= last; tok += 4) any |= a.mask[(int64_t)(q.q0 + tok) * a.mask_stride + c];
+    all = begin + w <= last ? ~0u : 0u;
+    if (c >= words) {
+      all = 0;
+      return;
+    }
+    const uint32_t* at = a.mask + (int64_t)(q.q0 + begin + w) * a.mask_stride + c;
+#pragma unroll 16
+    for (int tok = begin + w; tok <= last; tok += WAVES, at += WAVES * a.mask_stride) {
+      const uint32_t b = *at;
+      any |= b;
+      all &= b;
+    }
     const int left = q.n - 32 * c;
-    if (left < 32) any &= (1u << left) - 1;
+    if (left < 32) {
+      any &= (1u << left) - 1;
+      all &= (1u << left) - 1;
+    }
     if (any) {
       lo = min(lo, 32 * c + __ffs(any) - 1);
       hi = 32 * c + 32 - __clz(any);
     }
+  };
+#pragma unroll
+  for (int k = 0; k < HULL_KEPT; ++k) scan(64 * k + lane, kept[k]);
+  for (int c = 64 * HULL_KEPT + lane; c < words; c += 64) {
+    uint32_t all;
+    scan(c, all);
   }
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
@@ -1175,14 +1226,34 @@ __global__ __launch_bounds__(NT) void tree_hull_kernel(const RaggedArgs a, const
     hi = max(hi, __shfl_xor(hi, k, 64));
   }
   if (lane == 0) {
-    lo_of[w] = lo;
-    hi_of[w] = hi;
+    of[0][w] = lo;
+    of[1][w] = hi;
   }
   __syncthreads();
+#pragma unroll
+  for (int k = 0; k < WAVES; ++k) {
+    lo = min(lo, of[0][k]);
+    hi = max(hi, of[1][k]);
+  }
+  if (hi == 0) lo = 0;
+  // the first token from lo on that not all of the wavefront's tokens see (a wavefront without tokens has no say)
+  int whole = 32 * 64 * HULL_KEPT;
+#pragma unroll
+  for (int k = 0; k < HULL_KEPT; ++k) {
+    const int base = 32 * (64 * k + lane);
+    const uint32_t before = lo <= base ? 0u : (lo - base >= 32 ? ~0u : (1u << (lo - base)) - 1);
+    const uint32_t zero = ~(kept[k] | before);
+    if (zero) whole = min(whole, base + __ffs(zero) - 1);
+  }
+  if (begin + w > last) whole = INT32_MAX;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) whole = min(whole, __shfl_xor(whole, k, 64));
+  if (lane == 0) of[2][w] = whole;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    hi = max(max(hi_of[0], hi_of[1]), max(hi_of[2], hi_of[3]));
-    hull[2 * x] = hi ? min(min(lo_of[0], lo_of[1]), min(lo_of[2], lo_of[3])) : 0;
-    hull[2 * x + 1] = hi;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) whole = min(whole, of[2][k]);
+    hull[x] = Hull{lo, hi, whole};
   }
 }
 
@@ -1193,7 +1264,7 @@ hipError_t launch(const RaggedArgs& a, const Parts& pt, const RaggedPlan& p, hip
   else if (p.rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, KEYS, FP8, 2>), grid, block, 0, s, a, pt);
   else if (p.groups == 1) {
     if (KEYS == TREE && pt.hull) {
-      hipLaunchKernelGGL(tree_hull_kernel, dim3((unsigned)pt.tiles), block, 0, s, a, pt, const_cast<int32_t*>(pt.hull));
+      hipLaunchKernelGGL(tree_hull_kernel, dim3((unsigned)pt.tiles), dim3(HULL_NT), 0, s, a, pt, const_cast<Hull*>(pt.hull));
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
@@ -1221,7 +1292,7 @@ inline Parts make_parts(const RaggedArgs& a, const RaggedPlan& p, void* ws) {
   pt.by_splits = fast_div(p.splits);
   pt.by_tiles = fast_div(pt.tiles);
   pt.by_heads = fast_div(a.Hkv);
-  if (p.hull) pt.hull = reinterpret_cast<const int32_t*>(static_cast<char*>(ws) + ragged_parts_bytes(p, a.T, a.Hq, a.Dh));
+  if (p.hull) pt.hull = reinterpret_cast<const Hull*>(static_cast<char*>(ws) + ragged_parts_bytes(p, a.T, a.Hq, a.Dh));
   return pt;
 }
 

@@ -115,7 +115,7 @@ inline size_t ragged_parts_bytes(const RaggedPlan& p, int64_t T, int64_t Hq, int
   return p.splits <= 1 ? 0 : ragged_ml_bytes(p, T, Hq) + (size_t)T * Hq * p.splits * Dh * 4;
 }
 inline size_t ragged_ws_bytes(const RaggedPlan& p, int64_t T, int64_t Hq, int64_t Dh, int64_t tiles = 0) {
-  return ragged_parts_bytes(p, T, Hq, Dh) + (p.hull ? (size_t)tiles * 8 : 0);
+  return ragged_parts_bytes(p, T, Hq, Dh) + (p.hull ? (size_t)tiles * 12 : 0);
 }
 
 }  // namespace wam

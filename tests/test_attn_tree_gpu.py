@@ -141,7 +141,8 @@ def test_long_masks(lens, Hq, Hkv, Dh, fp8):
     kinds = {
         "branches": lambda n: i[n][:, None] * 2 // n == i[n] * 2 // n, "late": lambda n: (i[n] >= n - 40) & (i[n][:, None] % 3 > 0),
         "early": lambda n: (i[n] < 5) & (i[n][:, None] < 2000), "none": lambda n: np.zeros((n, n), bool), "self": lambda n: np.eye(n, dtype=bool),
-        "apart": lambda n: (i[n] % 1100 == 7) & (i[n] <= i[n][:, None])}
+        "apart": lambda n: (i[n] % 1100 == 7) & (i[n] <= i[n][:, None]), "causal": lambda n: i[n] <= i[n][:, None],
+        "all": lambda n: np.ones((n, n), bool), "shifted": lambda n: (i[n] >= 77) & (i[n] < n - 90) & (i[n][:, None] >= 0)}
     for name, sees in kinds.items():
         mask = np.zeros((b.T, max(-(-n // 32) for n, _ in lens)), np.int32)
         for at, (n, _) in zip(b.q_start, lens):
@@ -149,7 +150,7 @@ def test_long_masks(lens, Hq, Hkv, Dh, fp8):
             mask[at:at + n, :rows.shape[1]] = rows
         log(f"tree long masks {lens} Hq={Hq} Dh={Dh} fp8={fp8} {name}")
         check(run_tree(b, mask), expected(b, mask), name)
-    table = b.table.copy()
+    table = b.table.copy()  # (the last kind: new tokens from the 78th on, seen by all)
     b.table[0, 20:60] = -1
     check(run_tree(b, mask), expected(b, mask), "absent")
     b.table = table

@@ -50,7 +50,7 @@ def test_every_plan_covers_the_keys_and_can_be_joined():
         assert p["keys"] % 128 == 0 and p["keys"] >= 128 and p["keys"] * p["splits"] >= max_k
         assert (p["splits"] - 1) * p["keys"] < max(max_k, 1)
         assert p["groups"] == 1 or (p["rows"] == 128 and R == 1)
-        hull = 8 * p["tiles"] if p["hull"] else 0
+        hull = 12 * p["tiles"] if p["hull"] else 0
         assert p["ws"] == hull if p["splits"] == 1 else p["ws"] >= T * Hq * p["splits"] * (Dh * 4 + 8) + hull
         assert not p["hull"] or (p["rows"] == 128 and p["groups"] == 1)
         # every (row tile, part, head) has its workgroup
