@@ -530,7 +530,8 @@ typedef struct {
  *   2. The pages that are missing (entries [held, need)) are taken from its top, in the same order; an
  *      entry for which the stack holds no page any more becomes -1 (status[0] counts them).
  * (Pages for kept tokens that the request does not hold are taken like the new ones, with whatever they
- * hold.  A page belongs to one request: to share one, its owners keep it out of held and the stack.)
+ * hold.  A page belongs to one request: to share one, its owners keep it out of held and the stack, or no request has surplus
+ * pages: wam_page_collect.)
  * Written: block_table entries [held, need); free_list entries [n_free, n_free_out); and
  *   held_out [R]   pages that each request holds now;   n_free_out [1]
  *   q_start [R+1]  first row of each request among the new tokens, packed in request order
@@ -705,7 +706,8 @@ wam_status wam_page_collect(const wam_page_collect_desc* desc, const int32_t* ca
  * Request r's n = q_len[r] new tokens are the last of its kv_len[r]; it keeps m = n_keep[r] of them, numbers keep[q_start[r] + i],
  * i < m, ascending.  Row kv_len - n + keep[i] of its K, V and exponents goes to kv_len - n + i, all of them as they
  * were before the call; the rows past kv_len - n + m keep what they hold.  (The path of wam_verify_tree is such a list.)
- * Numbers outside (i, n) (in a list that does not ascend, those below their place) and rows of absent pages are left out. The rows' pages may belong to no other request. */
+ * Numbers outside (i, n) (in a list that does not ascend, those below their place) and rows of absent pages are left out.
+ * The rows' pages may belong to no other request. */
 typedef struct {
   int32_t R, T, max_pages;
   int64_t table_stride;
@@ -746,11 +748,11 @@ wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* 
  *   u[x] s Q(x) < R(x),
  * where R = P and s = 1 at first, and each rejection replaces R by max(R - s Q, 0) and s by its sum (drawn = 0: Q is a one at x,
  * so R loses the rejected token).  When no child is left, next_token is drawn from R: the first v with R_0 + .. + R_v >
- * u_next[r] * (the sum of R) (the last with R_v > 0 if rounding leaves none); from P where the sum of R is 0, -1 where that is 0 too.  With
- * one-hot rows this is greedy verification.
- * u [T], u_next [R] in [0, 1) are the caller's random numbers.  Sums are in fp64.  Entries of p that are negative or NaN count as 0.  A
- * node whose parent does not lie before it or whose token is outside [0, V) is never taken; nor is one past the
- * first WAM_TREE_MAX_NODES of a request.
+ * u_next[r] * (the sum of R) (the last with R_v > 0 if rounding leaves none); from P where the sum of R is 0, -1 where that
+ * is 0 too.  With one-hot rows this is greedy verification.
+ * u [T], u_next [R] in [0, 1) are the caller's random numbers.  Sums are in fp64.  Entries of p and q that are negative or NaN
+ * count as 0; infinite ones leave the outputs unspecified, but in their ranges.  A node whose parent does not lie before it or whose
+ * token is outside [0, V) is never taken; nor is one past the first WAM_TREE_MAX_NODES of a request.
  * Written: path [T]: from entry q_start[r] on the n_path[r] nodes taken, the root first (entries past them are left as they
  *   were): the list that wam_cache_compact takes; next_token [R]; and cache_len [R] = kv_len - q_len + n_path (both or
  *   neither given).  A request without rows: n_path 0, next_token -1.

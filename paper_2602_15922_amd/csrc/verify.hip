@@ -57,7 +57,7 @@ WAM_DEV void load_nodes(const VerifyArgs& a, const Tree& t, Nodes& x, float2* ke
     const bool ok = i > 0 && (unsigned)par < (unsigned)i && (unsigned)tok < (unsigned)a.d.V;
     if (FROM == ROWS && ok) {
       pq.x = a.p[(int64_t)(t.q0 + par) * a.d.p_stride + tok];
-      if (DRAWN) pq.y = a.q[(int64_t)(t.q0 + par) * a.d.q_stride + tok];
+      if (DRAWN) pq.y = fmaxf(a.q[(int64_t)(t.q0 + par) * a.d.q_stride + tok], 0.f);
     }
     x.parent[i] = ok ? par : -1;
     x.token[i] = tok;
@@ -68,10 +68,10 @@ WAM_DEV void load_nodes(const VerifyArgs& a, const Tree& t, Nodes& x, float2* ke
   }
 }
 
-// what is left of a probability (NaN and negative ones count as 0)
+// what is left of a probability (NaN and negative ones of either count as 0)
 WAM_DEV double left_of(float p, float q, double c) {
 #pragma clang fp contract(off)
-  const double x = (double)p - c * (double)q;
+  const double x = (double)p - c * (double)fmaxf(q, 0.f);
   return x > 0.0 ? x : 0.0;
 }
 WAM_DEV double left_of(float p) { return p > 0.f ? (double)p : 0.0; }

@@ -183,6 +183,9 @@ def test_probabilities_that_are_none():
         log("verify NaN entries")
         check(p, None, [0, 1, 2], [-1, 0, 0], np.zeros(3), [u], [0, 3])
         check(p, None, [0, 1, 3], [-1, 0, 0], np.full(3, 0.7), [u], [0, 3])
+        q = np.array([[0.75, -0.5, 0.25, np.nan]] * 3, np.float32)
+        for tokens in ([0, 0, 1], [0, 3, 0], [0, 2, 2]):
+            check(p, q, tokens, [-1, 0, 0], np.full(3, 0.9), [u], [0, 3])
 
 
 def test_padded_and_starts_out_of_range():
