@@ -179,7 +179,7 @@ __global__ __launch_bounds__(COPY_NT) void page_copy_kernel(const PageCopyArgs a
 // the same), so it knows how many free pages lie below its share of the pool and lists its own; one launch does
 // it and none waits for another.  Pools of more bytes than LDS has go by segments, from the first on.
 // Bound by the instructions that one CU issues for all marks (16 wavefronts, 4 cycles each): so no lane is masked off, 8 rows' first 64
-// entries are on their way at once and then a longer row's, 512 at a time.  1000 requests that keep 0 to 667 pages, 144700 pages: 28 us;
+// entries are on their way at once and then a longer row's, 512 at a time.  1000 requests that keep 0 to 1000 pages, 80000 of 144700 together: 28 us;
 // with lanes masked 40, a wavefront per row with atomic marks of a bit 44; 12 requests, 2224 pages 8.
 // ---------------------------------------------------------------------------------
 constexpr int COLLECT_NT = 1024, COLLECT_SMALL = 32 << 10, COLLECT_LARGE = 152 << 10;
