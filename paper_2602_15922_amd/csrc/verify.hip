@@ -244,15 +244,15 @@ __global__ __launch_bounds__(SUM_NT) void verify_sum_kernel(const VerifyArgs a, 
   if (tid == 0) a.sums[((int64_t)round * a.d.R + r) * a.slices + slice] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// One workgroup per request: ends the walk (passes that are still needed are its own), and draws the last token.
-constexpr int END_NT = 1024;
+// One workgroup per request: ends the walk (passes that are still needed are its own), and draws the last token.  Its
+// chain of loads is what takes the time, so it is small where no pass can be left.
 template <bool DRAWN>
-__global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) {
+__global__ __launch_bounds__(DRAWN ? 1024 : 256) void verify_end_kernel(const VerifyArgs a) {
+  constexpr int END_NT = DRAWN ? 1024 : 256, QUADS = SLICE / (4 * END_NT);  // fours of a slice's entries per thread
   __shared__ Nodes x;
   __shared__ uint32_t gone[SLICE / 32];
   __shared__ double part[END_NT / 64], own[WAM_VERIFY_MAX_VOCAB / SLICE];
   __shared__ int found, last_of[END_NT / 64];
-  static_assert(SLICE == 4 * END_NT, "a slice is four entries per thread");
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   VerifyState st = a.state[(int64_t)(a.rounds - 1) * a.d.R + r];  // (of a request without rows: anything)
   const float u_next = a.u_next[r];
@@ -321,11 +321,16 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
     const int v0 = slice * SLICE;
     const bool marked = !DRAWN && !whole_p && st.next > 1;
     if (marked) mark_gone<END_NT>(x, t.n, st, v0, gone);
-    double y[4];
-    f32x4 p, q;
-    load_pq<DRAWN>(a, t.q0 + st.cur, v0 + 4 * tid, !whole_p && st.c != 0.0, p, q);
-    left4<DRAWN>(p, q, st.c, marked ? gone : nullptr, 4 * tid, y);
-    const double mine = (y[0] + y[1]) + (y[2] + y[3]), incl = wave_scan_f64(mine);
+    double y[4 * QUADS], mine = 0.0;
+    f32x4 p[QUADS], q[QUADS];
+#pragma unroll
+    for (int k = 0; k < QUADS; ++k) load_pq<DRAWN>(a, t.q0 + st.cur, v0 + 4 * (QUADS * tid + k), !whole_p && st.c != 0.0, p[k], q[k]);
+#pragma unroll
+    for (int k = 0; k < QUADS; ++k) {
+      left4<DRAWN>(p[k], q[k], st.c, marked ? gone : nullptr, 4 * (QUADS * tid + k), y + 4 * k);
+      mine += (y[4 * k] + y[4 * k + 1]) + (y[4 * k + 2] + y[4 * k + 3]);
+    }
+    const double incl = wave_scan_f64(mine);
     if (tid == 0) found = INT32_MAX;
     if (lane == 63) part[w] = incl;
     __syncthreads();
@@ -333,10 +338,10 @@ __global__ __launch_bounds__(END_NT) void verify_end_kernel(const VerifyArgs a) 
     for (int k = 0; k < w; ++k) sum += part[k];
     int first = INT32_MAX, last = -1;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 4 * QUADS; ++e) {
       sum += y[e];
       if (y[e] > 0.0) {
-        last = v0 + 4 * tid + e;
+        last = v0 + 4 * QUADS * tid + e;
         if (sum > goal && first == INT32_MAX) first = last;
       }
     }
@@ -370,7 +375,7 @@ hipError_t launch(const VerifyArgs& a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(verify_end_kernel<DRAWN>, dim3((unsigned)a.d.R), dim3(END_NT), 0, s, a);
+  hipLaunchKernelGGL(verify_end_kernel<DRAWN>, dim3((unsigned)a.d.R), dim3(DRAWN ? 1024 : 256), 0, s, a);
   return hipGetLastError();
 }
 

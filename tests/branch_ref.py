@@ -118,34 +118,35 @@ def verify(p, q, tokens, parent, u, u_next, max_nodes=1024):
     if n == 0:
         return [], -1
     F = lambda x: Fraction(float(x)) if x > 0 else Fraction(0)  # noqa: E731
+    row = lambda x: {int(v): Fraction(float(x[v])) for v in np.flatnonzero(np.asarray(x) > 0)}  # noqa: E731
     V = len(p[0])
     cur, path = 0, [0]
-    left, s = None, Fraction(1)  # left: what is left of the target where it is no longer p itself
+    left, s = None, Fraction(1)  # left: what is left of the target (entries above 0) where it is no longer p itself
     for i in range(1, min(n, max_nodes)):
         x = int(tokens[i])
         if int(parent[i]) != cur or not 0 <= x < V:
             continue
-        now = left if left is not None else [F(v) for v in p[cur]]
+        chance = left.get(x, Fraction(0)) if left is not None else F(p[cur][x])
         draft = F(q[cur][x]) if q is not None else Fraction(1)
-        if Fraction(float(u[i])) * s * draft < now[x]:
+        if Fraction(float(u[i])) * s * draft < chance:
             cur, left, s = i, None, Fraction(1)
             path.append(i)
-        elif q is not None:
-            left = [max(a - s * F(b), 0) for a, b in zip(now, q[cur])]
-            s = sum(left)
+            continue
+        left = row(p[cur]) if left is None else left
+        if q is not None:
+            left = {v: a - s * F(q[cur][v]) for v, a in left.items()}
+            left = {v: a for v, a in left.items() if a > 0}
+            s = sum(left.values())
         else:
-            s -= now[x]
-            left = list(now)
-            left[x] = Fraction(0)
-    now = left if left is not None else [F(v) for v in p[cur]]
-    if sum(now) == 0:
-        now = [F(v) for v in p[cur]]
-    total = sum(now)
+            s -= chance
+            left.pop(x, None)
+    left = row(p[cur]) if not left else left
+    total = sum(left.values())
     if total == 0:
         return path, -1
     goal, at = Fraction(float(u_next)) * total, Fraction(0)
-    for v in range(V):
-        at += now[v]
+    for v in sorted(left):
+        at += left[v]
         if at > goal:
             return path, v
-    return path, max(v for v in range(V) if now[v] > 0)
+    return path, max(left)

@@ -129,8 +129,8 @@ def bits_of(sees):
     return np.packbits(out, axis=1, bitorder="little").view(np.int32)
 
 
-@pytest.mark.parametrize("lens,Hq,Hkv,Dh,fp8", [([(2600, 2700), (40, 300)], 1, 1, 64, False), ([(2500, 2531), (70, 70)], 2, 1, 128, False),
-                                                ([(2300, 2900), (3, 100)], 1, 1, 128, True), ([(1300, 1400), (1290, 1290), (1500, 3000)], 1, 1, 64, False)])
+@pytest.mark.parametrize("lens,Hq,Hkv,Dh,fp8", [([(2600, 2700), (40, 300)], 1, 1, 64, False), ([(1500, 1531), (70, 70)], 2, 1, 128, False),
+                                                ([(1700, 2300), (3, 100)], 1, 1, 128, True), ([(1300, 1400), (1290, 1290), (1500, 3000)], 1, 1, 64, False)])
 def test_long_masks(lens, Hq, Hkv, Dh, fp8):
     """Masks of thousands of tokens, whose rows see nothing of long stretches: before their own branch, behind it, or of all new
     tokens; with pages missing, and values that are not finite in what is not seen."""
