@@ -759,6 +759,27 @@ def wam_attn_tree(cache: wam_paged_cache, q, block_table, q_start, kv_len, mask,
                                *_workspace(dev, ws), _stream_on(stream, dev)))
 
 
+_f32 = None
+
+
+def _floats(dev, rows, p, q, u, u_next):
+    """Probabilities (q may be None) of rows = (T, V), rows contiguous, and random numbers, one for each row and any, contiguous:
+    fp32 on device number dev."""
+    global _f32
+    if _f32 is None:
+        import torch
+        _f32 = torch.float32
+    f32 = _f32
+    if p.dtype is f32 and u.dtype is f32 and u_next.dtype is f32 and u.get_device() == dev == u_next.get_device() and \
+            u.shape == rows[:1] and u.is_contiguous() and u_next.is_contiguous() and (p.stride(1) == 1 or rows[1] == 1) and \
+            (q is None or (q.dtype is f32 and q.get_device() == dev and q.shape == rows and (q.stride(1) == 1 or rows[1] == 1))):
+        return
+    for name, t, shape in (("p", p, rows), ("q", q, rows), ("u", u, rows[:1]), ("u_next", u_next, u_next.shape)):
+        if t is not None and (t.dtype is not f32 or t.get_device() != dev or t.shape != shape or
+                              (t.stride(-1) != 1 and t.shape[-1] > 1)):
+            raise ValueError(f"{name} must be an fp32 tensor {list(shape)} of contiguous rows on the call's device, " + _got(t))
+
+
 def wam_verify_tree_workspace_bytes(R: int, T: int, V: int, drawn: bool) -> int:
     d = wam_verify_tree_desc(R, T, V, int(drawn), V, V)
     return lib().wam_verify_tree_workspace_bytes(C.byref(d))
@@ -769,24 +790,22 @@ def wam_verify_tree(p, q, tokens, parent, u, u_next, q_start, path, n_path, next
     """p [T, V] fp32 (rows at any stride); q likewise where the drafts were drawn, else None; u [T], u_next [R] contiguous
     fp32; tokens, parent, path [T], q_start [R + 1], n_path, next_token, q_len, kv_len and cache_len [R] contiguous int32 (the
     last three may be None); ws of wam_verify_tree_workspace_bytes(R, T, V, drawn)."""
-    import torch
-    (T, V), R, dev, f32 = p.shape, u_next.shape[0], p.get_device(), torch.float32
-    for name, t, shape in (("p", p, (T, V)), ("q", q, (T, V)), ("u", u, (T,)), ("u_next", u_next, (R,))):
-        if t is not None and (t.dtype is not f32 or t.get_device() != dev or t.shape != shape or
-                              (t.stride(-1) != 1 and t.shape[-1] > 1)):
-            raise ValueError(f"{name} must be an fp32 tensor {list(shape)} of contiguous rows on the call's device, " + _got(t))
+    (T, V), (R,), dev = p.shape, u_next.shape, p.get_device()
+    _floats(dev, (T, V), p, q, u, u_next)
     names, sizes = "tokens parent q_start path n_path next_token", (T, T, R + 1, T, R, R)
-    ints, given = (tokens, parent, q_start, path, n_path, next_token), []
-    for name, t in (("q_len", q_len), ("kv_len", kv_len), ("cache_len", cache_len)):
-        if t is not None:
-            names, sizes, ints = f"{names} {name}", sizes + (R,), ints + (t,)
-            given.append(name)
+    ints = tokens, parent, q_start, path, n_path, next_token
+    if kv_len is not None and cache_len is not None:
+        names, sizes, ints = names + " kv_len cache_len", sizes + (R, R), ints + (kv_len, cache_len)
+    elif kv_len is not None or cache_len is not None:
+        raise ValueError("kv_len and cache_len must be given both or neither")
+    if q_len is not None:
+        names, sizes, ints = names + " q_len", sizes + (R,), ints + (q_len,)
     tokens, parent, q_start, path, n_path, next_token, *lens = _ints(dev, names, sizes, ints)
-    lens = dict(zip(given, lens))
-    d = wam_verify_tree_desc(R, T, V, int(q is not None), max(p.stride(0), V), V if q is None else max(q.stride(0), V))
-    _check(lib().wam_verify_tree(C.byref(d), p.data_ptr(), _p(q), tokens, parent, u.data_ptr(), u_next.data_ptr(), q_start,
-                                 lens.get("q_len"), lens.get("kv_len"), path, n_path, next_token, lens.get("cache_len"),
-                                 *_workspace(dev, ws), _stream_on(stream, dev)))
+    q_len = lens.pop() if q_len is not None else None
+    kv_len, cache_len = lens or (None, None)
+    d = wam_verify_tree_desc(R, T, V, 0 if q is None else 1, max(p.stride(0), V), V if q is None else max(q.stride(0), V))
+    _check(lib().wam_verify_tree(C.byref(d), p.data_ptr(), _p(q), tokens, parent, u.data_ptr(), u_next.data_ptr(), q_start, q_len,
+                                 kv_len, path, n_path, next_token, cache_len, *_workspace(dev, ws), _stream_on(stream, dev)))
 
 
 def wam_tree_mask(parent, words=None):
