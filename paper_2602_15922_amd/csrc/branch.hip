@@ -322,12 +322,12 @@ __global__ __launch_bounds__(COLLECT_NT) void page_collect_kernel(const PageColl
 // ---------------------------------------------------------------------------------
 // Compact.  A workgroup owns one head of K or V of a request.  Row i's new place lies below what it holds (others are left
 // out), so a group of rows overwrites nothing that a later one reads, and its own loads end before its stores.
-// Bound by memory where lists are long (a group of 256 rows of 256 bytes, 64 KB, is on its way while the one before is stored;
+// Bound by memory where lists are long (a group of 128 rows of 256 bytes, 32 KB, is on its way while the one before is stored;
 // the rows' places are looked up 1024 at a time), by the chain lengths -> numbers -> table -> row where they are short.  4 x 1576
-// of 3152 rows, 40 heads: 69 us for 258 MB (3.7 TB/s); 128 rows at a time, looked up as they are moved, 166.  16 paths of 2 to 6
-// rows, 8 heads 4.0.
+// of 3152 rows, 40 heads: 68 us for 258 MB (3.8 TB/s; groups of 256 rows 69.5, heads in a row on one XCD 68, marked as used once
+// 69.5); looked up as they are moved, nothing ahead, 166.  16 paths of 2 to 6 rows, 8 heads 3.9.
 // ---------------------------------------------------------------------------------
-constexpr int MOVE_NT = 256, MOVE_PER = 16, MOVE_ROWS = 1024;
+constexpr int MOVE_NT = 256, MOVE_PER = 8, MOVE_ROWS = 1024;
 
 template <int CPR>  // 16-byte chunks of a row
 __global__ __launch_bounds__(MOVE_NT) void cache_compact_kernel(const CacheCompactArgs a) {

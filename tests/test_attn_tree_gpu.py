@@ -130,7 +130,8 @@ def bits_of(sees):
 
 
 @pytest.mark.parametrize("lens,Hq,Hkv,Dh,fp8", [([(2600, 2700), (40, 300)], 1, 1, 64, False), ([(1500, 1531), (70, 70)], 2, 1, 128, False),
-                                                ([(1700, 2300), (3, 100)], 1, 1, 128, True), ([(1300, 1400), (1290, 1290), (1500, 3000)], 1, 1, 64, False)])
+                                                ([(1700, 2300), (3, 100)], 1, 1, 128, True), ([(1300, 1400), (1290, 1290), (1500, 3000)], 1, 1, 64, False),
+                                                ([(1300, 1400)], 24, 24, 64, False)])
 def test_long_masks(lens, Hq, Hkv, Dh, fp8):
     """Masks of thousands of tokens, whose rows see nothing of long stretches: before their own branch, behind it, or of all new
     tokens; with pages missing, and values that are not finite in what is not seen."""
@@ -144,6 +145,8 @@ def test_long_masks(lens, Hq, Hkv, Dh, fp8):
         "apart": lambda n: (i[n] % 1100 == 7) & (i[n] <= i[n][:, None]), "causal": lambda n: i[n] <= i[n][:, None],
         "all": lambda n: np.ones((n, n), bool), "shifted": lambda n: (i[n] >= 77) & (i[n] < n - 90) & (i[n][:, None] >= 0)}
     for name, sees in kinds.items():
+        if Hq > 2 and name not in ("late", "branches", "shifted"):
+            continue
         mask = np.zeros((b.T, max(-(-n // 32) for n, _ in lens)), np.int32)
         for at, (n, _) in zip(b.q_start, lens):
             rows = bits_of(sees(n))
