@@ -557,6 +557,12 @@ def _heads(dev, name, t, rows):
     return t.data_ptr(), stride[0]
 
 
+def _apart(t, rows, width):
+    """Row stride of a tensor of which `rows` rows are read (the stride of a single one says nothing).  Rows that overlap,
+    as expand makes them, keep theirs, and the library refuses it."""
+    return t.stride(0) if rows > 1 else width
+
+
 def _workspace(dev, ws):
     """Address and bytes."""
     if ws is None:
@@ -737,7 +743,7 @@ def wam_attn_tree_workspace_bytes(cache: wam_paged_cache, R: int, T: int, Hq: in
 
 def wam_attn_tree(cache: wam_paged_cache, q, block_table, q_start, kv_len, mask, o, ws=None, max_kv=None, q_len=None,
                   scale=0.0, stream=None):
-    """As wam_attn_paged, with mask [T, words] int32 (or more rows; a row's words contiguous): bit j % 32 of word j / 32 of a
+    """As wam_attn_paged, with mask [T, words] int32 (or more rows, none overlapping; a row's words contiguous): bit j % 32 of word j / 32 of a
     row says whether it sees its request's new token j.  ws: wam_attn_tree_workspace_bytes(cache, R, T, Hq, max_kv)."""
     (T, Hq, _), dev, (R, width) = q.shape, q.get_device(), block_table.shape
     rows = T, Hq, cache.Dh
@@ -754,7 +760,7 @@ def wam_attn_tree(cache: wam_paged_cache, q, block_table, q_start, kv_len, mask,
         q_start, kv_len, q_len = _ints(dev, "q_start kv_len q_len", (R + 1, R, R), (q_start, kv_len, q_len))
     _cache_on(cache, dev)
     d = wam_attn_tree_desc(R, T, Hq, width, min(width * cache.page_size, 1 << 30) if max_kv is None else max_kv, words,
-                           stride, q_stride, o_stride, max(bits[0], words), scale)
+                           stride, q_stride, o_stride, _apart(mask, T, words), scale)
     _check(lib().wam_attn_tree(C.byref(d), C.byref(cache), qp, table, q_start, q_len, kv_len, mask.data_ptr(), op,
                                *_workspace(dev, ws), _stream_on(stream, dev)))
 
@@ -787,7 +793,7 @@ def wam_verify_tree_workspace_bytes(R: int, T: int, V: int, drawn: bool) -> int:
 
 def wam_verify_tree(p, q, tokens, parent, u, u_next, q_start, path, n_path, next_token, ws, q_len=None, kv_len=None,
                     cache_len=None, stream=None):
-    """p [T, V] fp32 (rows at any stride); q likewise where the drafts were drawn, else None; u [T], u_next [R] contiguous
+    """p [T, V] fp32 (rows at any stride >= V); q likewise where the drafts were drawn, else None; u [T], u_next [R] contiguous
     fp32; tokens, parent, path [T], q_start [R + 1], n_path, next_token, q_len, kv_len and cache_len [R] contiguous int32 (the
     last three may be None); ws of wam_verify_tree_workspace_bytes(R, T, V, drawn)."""
     (T, V), (R,), dev = p.shape, u_next.shape, p.get_device()
@@ -803,7 +809,7 @@ def wam_verify_tree(p, q, tokens, parent, u, u_next, q_start, path, n_path, next
     tokens, parent, q_start, path, n_path, next_token, *lens = _ints(dev, names, sizes, ints)
     q_len = lens.pop() if q_len is not None else None
     kv_len, cache_len = lens or (None, None)
-    d = wam_verify_tree_desc(R, T, V, 0 if q is None else 1, max(p.stride(0), V), V if q is None else max(q.stride(0), V))
+    d = wam_verify_tree_desc(R, T, V, 0 if q is None else 1, _apart(p, T, V), V if q is None else _apart(q, T, V))
     _check(lib().wam_verify_tree(C.byref(d), p.data_ptr(), _p(q), tokens, parent, u.data_ptr(), u_next.data_ptr(), q_start, q_len,
                                  kv_len, path, n_path, next_token, cache_len, *_workspace(dev, ws), _stream_on(stream, dev)))
 
