@@ -659,7 +659,8 @@ wam_status wam_attn_cross(const wam_attn_cross_desc* desc, const void* q, const 
  * these tokens fill are shared: table[dst][j] = table[src][first + j], j < w = floor(len / page_size).  The last, if it is
  * filled in part, gets a page of its own, the forks' in their order from the top of the stack: table[dst][w]; copies[i] = (source
  * page, that page, len % page_size rows) says what wam_page_copy has to copy, (-1, -1, 0) where there is nothing.  With no page
- * on the stack any more the entry is -1 (an absent page).
+ * on the stack any more the entry is -1 (an absent page).  An absent page of the source is absent in the fork: its entry is
+ * shared, the last one's too (no page is taken for it, and it counts as held, as in the source).
  * A fork with src or dst outside [0, R), a dst that holds pages or that an earlier fork names, first or len negative, or tokens
  * past the pages that src holds, does nothing.
  * Written: the table's entries named above; copies [N][3]; and

@@ -34,6 +34,8 @@ constexpr int FORK_NT = 256;
 
 struct Fork {
   int src, dst, first, whole, tail;
+  int last;    // the source's entry of the tail's page
+  bool takes;  // it needs a page of its own: of an absent page there is nothing to copy, and its entry is shared
 };
 
 template <int E>  // forks per thread: N <= 256 E
@@ -58,6 +60,8 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
     if ((int64_t)f.first * ps + len > (int64_t)held(f.src) * ps) return false;
     f.whole = fdiv(a.ps, len);
     f.tail = len - f.whole * ps;
+    f.last = f.tail > 0 ? a.table[f.src * a.d.table_stride + f.first + f.whole] : -1;  // (a source's row is not written)
+    f.takes = (unsigned)f.last < (unsigned)a.d.n_pages;
     return true;
   };
   int tails = 0, bad = 0;
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
     const bool ok = i < N && get(i, f);
     bad += i < N && !ok;
     if (i < N) at[i] = ok ? tails : -1;
-    tails += ok && f.tail > 0;
+    tails += ok && f.takes;
   }
   const int incl = wave_scan(tails);
   const int bads = wave_scan(bad);
@@ -96,7 +100,7 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
       const int h = held(r), i = owner[r];
       wrong += h != a.held[r];
       Fork f;
-      a.held_out[r] = i < N && at[i] >= 0 && get(i, f) ? f.whole + (f.tail > 0 && at[i] < nf) : h;
+      a.held_out[r] = i < N && at[i] >= 0 && get(i, f) ? f.whole + (f.tail > 0 && (!f.takes || at[i] < nf)) : h;
     }
     __syncthreads();
     const int w2 = wave_scan(wrong);
@@ -115,23 +119,17 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
     const int i = (int)(item / chunks), part = (int)(item - (int64_t)i * chunks), j = part * FORK_NT + tid;
     Fork f;
     const bool ok = at[i] >= 0 && get(i, f);
-    int page = -1, last = -1;
+    const bool some = ok && f.tail > 0 && at[i] < nf, copied = some && f.takes;
+    const int top = some ? a.free_list[nf - 1 - at[i]] : -1, page = copied ? top : -1;  // (on its way with the tail's entry)
     if (ok) {
       const int32_t* from = a.table + (int64_t)f.src * a.d.table_stride + f.first;
       int32_t* to = a.table + (int64_t)f.dst * a.d.table_stride;
       if (j < f.whole) to[j] = from[j];
-      if (part == 0 && tid == 0 && f.tail > 0) {
-        if (at[i] < nf) {
-          page = a.free_list[nf - 1 - at[i]];
-          last = from[f.whole];
-        }
-        to[f.whole] = page;
-      }
+      if (part == 0 && tid == 0 && f.tail > 0) to[f.whole] = f.takes ? page : f.last;
     }
     if (part == 0 && tid == 0) {
-      const bool copied = ok && f.tail > 0 && at[i] < nf;
-      a.copies[3 * i] = copied ? last : -1;
-      a.copies[3 * i + 1] = copied ? page : -1;
+      a.copies[3 * i] = copied ? f.last : -1;
+      a.copies[3 * i + 1] = page;
       a.copies[3 * i + 2] = copied ? f.tail : 0;
     }
   }
