@@ -198,7 +198,7 @@ template <bool DRAWN, bool LATER>
 __global__ __launch_bounds__(SUM_NT) void verify_sum_kernel(const VerifyArgs a, int round) {
   __shared__ Nodes x;
   __shared__ uint32_t gone[SLICE / 32];
-  __shared__ double part[SUM_NT / 64];
+  __shared__ double part[SUM_NT];
   const int r = fdiv(a.by_slices, blockIdx.x), slice = blockIdx.x - r * a.slices, tid = threadIdx.x, w = tid >> 6;
   const int v0 = slice * SLICE;
   VerifyState st = first_state();
@@ -238,10 +238,11 @@ __global__ __launch_bounds__(SUM_NT) void verify_sum_kernel(const VerifyArgs a, 
     left4<DRAWN>(p[k], q[k], st.c, some ? gone : nullptr, 4 * (k * SUM_NT + tid), y);
     sum += (y[0] + y[1]) + (y[2] + y[3]);
   }
-  sum = wave_sum_f64(sum);
-  if ((tid & 63) == 0) part[w] = sum;
+  part[tid] = sum;
   __syncthreads();
-  if (tid == 0) a.sums[((int64_t)round * a.d.R + r) * a.slices + slice] = (part[0] + part[1]) + (part[2] + part[3]);
+  if (w > 0) return;
+  sum = wave_sum_f64((part[tid] + part[tid + 64]) + (part[tid + 128] + part[tid + 192]));
+  if (tid == 0) a.sums[((int64_t)round * a.d.R + r) * a.slices + slice] = sum;
 }
 
 // One workgroup per request: ends the walk (passes that are still needed are its own), and draws the last token.  Its
@@ -268,20 +269,24 @@ __global__ __launch_bounds__(DRAWN ? 1024 : 256) void verify_end_kernel(const Ve
   const double* sums = a.sums + ((int64_t)st.round * a.d.R + r) * a.slices;
   if (!DRAWN) load_nodes<DRAWN, END_NT, NONE>(a, t, x, nullptr);
   else if (!st.done) load_nodes<DRAWN, END_NT, KEPT>(a, t, x, nullptr);
-  // the sums of all slices, a wavefront for each
+  // the sums of all slices, a wavefront for each, in the order of verify_sum_kernel (s[j]: what a lane of its wavefront j adds
+  // up), so that it does not matter in which of the two a pass is made
   const auto sum_all = [&](bool whole_p) {
     for (int i = w; i < a.slices; i += END_NT / 64) {
-      double s = 0.0;
-#pragma unroll 8
-      for (int k = 0; k < SLICE / 256; ++k) {
-        double y[4];
-        f32x4 p, q;
-        load_pq<DRAWN>(a, t.q0 + st.cur, i * SLICE + 256 * k + 4 * lane, !whole_p && st.c != 0.0, p, q);
-        left4<DRAWN>(p, q, st.c, nullptr, 0, y);
-        s += (y[0] + y[1]) + (y[2] + y[3]);
-      }
-      s = wave_sum_f64(s);
-      if (lane == 0) own[i] = s;
+      double s[4] = {0.0, 0.0, 0.0, 0.0};
+      static_assert(SUM_NT == 4 * 64, "four wavefronts");
+#pragma unroll 2
+      for (int k = 0; k < SUM_PER; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          double y[4];
+          f32x4 p, q;
+          load_pq<DRAWN>(a, t.q0 + st.cur, i * SLICE + 4 * (k * SUM_NT + 64 * j + lane), !whole_p && st.c != 0.0, p, q);
+          left4<DRAWN>(p, q, st.c, nullptr, 0, y);
+          s[j] += (y[0] + y[1]) + (y[2] + y[3]);
+        }
+      const double sum = wave_sum_f64((s[0] + s[1]) + (s[2] + s[3]));
+      if (lane == 0) own[i] = sum;
     }
     __syncthreads();
     sums = own;
