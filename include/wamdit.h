@@ -744,7 +744,8 @@ wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* 
  * The nodes of request r are its rows; node 0, the root, is the last token that is already settled.  Node i > 0 stands for the
  * drafted tokens[q_start + i], a child of node parent[q_start + i], which must lie before it.  p [T] rows of V fp32: the target's
  * probabilities of the token after each node; q likewise the draft's, from which a node's children were drawn
- * independently (drawn = 1), or NULL where they were chosen and not drawn (drawn = 0, say a node's likeliest).
+ * independently (drawn = 1), or NULL where they were chosen and not drawn (drawn = 0, say a node's likeliest).  (With T = 0
+ * no tensor of rows needs an address.)
  * From the root on, the children of the present node are tried in order of their numbers: x is taken if
  *   u[x] s Q(x) < R(x),
  * where R = P and s = 1 at first, and each rejection replaces R by max(R - s Q, 0) and s by its sum (drawn = 0: Q is a one at x,

@@ -507,7 +507,8 @@ wam_status wam_verify_tree(const wam_verify_tree_desc* desc, const float* p, con
   CHECK(desc, WAM_EINVAL, "desc is NULL");
   const wam_verify_tree_desc& d = *desc;
   TRY(check_verify(d));
-  CHECK(!d.drawn == !q, WAM_EINVAL, "q must be given where drawn is 1 and only there");
+  // (without rows p and q have no address)
+  CHECK(!d.drawn == !q || (d.drawn && d.T == 0), WAM_EINVAL, "q must be given where drawn is 1 and only there");
   CHECK(!kv_len == !cache_len, WAM_EINVAL, "kv_len and cache_len must be given both or neither");
   if (d.R == 0) return WAM_OK;
   if (d.T > 0) {
