@@ -87,6 +87,15 @@ WAM_DEV int next_child(const Nodes& x, int n, int cur, int i) {
   return n;
 }
 
+// whether the token of child i of `cur` is an earlier child's (the same in all lanes)
+WAM_DEV bool tried(const Nodes& x, int cur, int i) {
+  const int lane = threadIdx.x & 63, token = x.token[i];
+  bool hit = false;
+#pragma unroll 4
+  for (int k = lane; k - lane < i; k += 64) hit |= k < i && x.parent[k] == cur && x.token[k] == token;
+  return __any(hit);
+}
+
 // The walk from a state whose s is known, to the next sum that it needs or to its end.  Taken nodes go to `path` (may be
 // NULL) from entry `count` on.
 template <bool DRAWN>
@@ -96,10 +105,7 @@ WAM_DEV void walk(const Nodes& x, int n, VerifyState& st, int32_t* path) {
     const int i = next_child(x, n, st.cur, st.next);
     if (i >= n) break;
     const double r = DRAWN ? left_of(x.p[i], x.q[i], st.c) : left_of(x.p[i]);
-    bool gone = false;
-    if (!DRAWN)  // (a token that was rejected here before)
-      for (int k = next_child(x, n, st.cur, 0); k < i; k = next_child(x, n, st.cur, k + 1)) gone |= x.token[k] == x.token[i];
-    const double chance = gone ? 0.0 : r;
+    const double chance = !DRAWN && tried(x, st.cur, i) ? 0.0 : r;  // (0: a token that was rejected here before)
     const bool take = (double)x.u[i] * st.s * (DRAWN ? (double)x.q[i] : 1.0) < chance;
     st.next = i + 1;
     if (take) {
