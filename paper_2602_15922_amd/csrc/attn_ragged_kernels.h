@@ -704,14 +704,28 @@ WAM_DEV void tile_arrived() {
   asm volatile("" ::: "memory");
 }
 
+// A workgroup's work: its request, KV head, first row, and keys.
+struct Work {
+  Req q;
+  int r, hk, G, m0, split, start, end;
+  int gap = INT32_MAX, past = INT32_MAX;  // tree: the tiles gap .. past - 1 are seen by no row (windows of 16 of them),
+  int seen = 1 << 30, past_seen = 0;      // the tiles seen .. past_seen - 1 by every row (none)
+  int meta;    // lane: page of a group of the first keys
+  bool whole;  // the request has one part: the output itself is written
+};
+
 // GROUPS = 2: the key tiles go in turn to two groups of four wavefronts, each with its own pair of LDS buffers, and the
 // groups' states are joined in LDS at the end: two wavefronts per SIMD where there are too few workgroups for two on a
 // CU, without parts in memory.
 // False, and nothing is written: V of keys that only some of the rows see holds values that are not finite.
 template <int DH, int KEYS, bool FP8, int GROUPS>
-WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Req& q, int r, int hk, int G, int m0, int split,
-                       bool whole, int start, int end, int meta, bf16* smem_all, int* odd, int gap, int past, int seen, int past_seen) {
+WAM_DEV bool tile_rows(const RaggedArgs& a, const Parts& pt, const Work& k, bf16* smem_all, int* odd) {
   constexpr int KS = DH / 16, MT = DH / 32, TILE = 2 * BN * DH;
+  const Req& q = k.q;
+  const int r = k.r, hk = k.hk, G = k.G, m0 = k.m0, split = k.split, start = k.start, end = k.end;
+  const int gap = k.gap, past = k.past, seen = k.seen, past_seen = k.past_seen;
+  const bool whole = k.whole;
+  int meta = k.meta;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5, l32 = lane & 31;
   const int w = uniform(tid >> 6) & 3, grp = GROUPS == 1 ? 0 : uniform(tid >> 8);
   bf16* smem = smem_all + grp * 2 * TILE;
@@ -961,15 +975,6 @@ WAM_DEV int find_request(const RaggedArgs& a, int x, int G, int shift, int lane)
   }
 }
 
-// A workgroup's work: its request, KV head, first row, and keys.
-struct Work {
-  Req q;
-  int r, hk, G, m0, split, start, end;
-  int gap, past;        // tree: the tiles gap .. past - 1 are seen by no row (windows of 16 of them),
-  int seen, past_seen;  // the tiles seen .. past_seen - 1 by every row
-  int meta;    // lane: page of a group of the first keys
-  bool whole;  // the request has one part: the output itself is written
-};
 template <int KEYS, int SHIFT>
 WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, int block, Work& k) {
   const int lane = threadIdx.x & 63;
@@ -1010,9 +1015,6 @@ WAM_DEV bool find_work(const RaggedArgs& a, const Parts& pt, int block, Work& k)
   const int kmax = kend_of<KEYS>(a, k.q, fdiv(a.group, last));
   k.end = kmax - k.start < pt.split_keys ? kmax : k.start + pt.split_keys;
   if constexpr (KEYS == TREE && SHIFT == 7) {
-    k.gap = k.past = INT32_MAX;
-    k.seen = 1 << 30;  // (none)
-    k.past_seen = 0;
     if (pt.hull) {
       const Hull h = pt.hull[x];
       const int64_t history = (int64_t)k.q.kv - k.q.n, first = history + h.first, past = history + h.past;
@@ -1055,8 +1057,7 @@ __global__ __launch_bounds__(NT * GROUPS, DH == 64 ? 3 : 2) void ragged_tile_ker
   if (!find_work<KEYS, 7>(a, pt, blockIdx.x, k)) return;
   int last = k.m0 + 1;  // streamed: the rows m0 .. last - 1, 32 at a time
   if (GROUPS == 2 || k.q.n * k.G > RAGGED_STREAM) {
-    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k.q, k.r, k.hk, k.G, k.m0, k.split, k.whole, k.start, k.end, k.meta, smem, odd, k.gap, k.past, k.seen, k.past_seen))
-      return;
+    if (tile_rows<DH, KEYS, FP8, GROUPS>(a, pt, k, smem, odd)) return;
     int block = blockIdx.x;  // (found anew, so that nothing is kept for it: two samples' 3152 rows 1861 -> 1831 us)
     asm volatile("" : "+s"(block) : : "memory");
     find_work<KEYS, 7>(a, pt, block, k);
@@ -1176,13 +1177,14 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(const RaggedArgs a, co
 // of them see it does not mask (two futures of 3152 rows over 6304 keys, 40 heads: 1563 us without, 1416 without the last, 1387; of
 // this 8).  A workgroup per row tile, its tokens in turn over the wavefronts, the masks' words over the lanes.
 constexpr int HULL_NT = 512, HULL_KEPT = 4;
+template <int KEYS>  // (a template, so that only the file of the trees holds it)
 __global__ __launch_bounds__(HULL_NT) void tree_hull_kernel(const RaggedArgs a, const Parts pt, Hull* hull) {
   constexpr int WAVES = HULL_NT / 64;
   __shared__ int of[3][WAVES];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), x = blockIdx.x, G = (int)a.group.d;
   const int r = uniform(find_request(a, x, G, 7, lane));
   if (r < 0) return;
-  const Req q = request<TREE>(a, r);
+  const Req q = request<KEYS>(a, r);
   const int64_t m0 = ((int64_t)x - r - (((int64_t)q.q0 * G) >> 7)) * RAGGED_ROWS;
   const int rows = q.n * G;
   if (m0 < 0 || m0 >= rows) return;
@@ -1263,10 +1265,12 @@ hipError_t launch(const RaggedArgs& a, const Parts& pt, const RaggedPlan& p, hip
   if (p.rows == 16) hipLaunchKernelGGL((ragged_stream_kernel<DH, KEYS, FP8, 1>), grid, block, 0, s, a, pt);
   else if (p.rows == 32) hipLaunchKernelGGL((ragged_stream_kernel<DH, KEYS, FP8, 2>), grid, block, 0, s, a, pt);
   else if (p.groups == 1) {
-    if (KEYS == TREE && pt.hull) {
-      hipLaunchKernelGGL(tree_hull_kernel, dim3((unsigned)pt.tiles), dim3(HULL_NT), 0, s, a, pt, const_cast<Hull*>(pt.hull));
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
+    if constexpr (KEYS == TREE) {
+      if (pt.hull) {
+        hipLaunchKernelGGL(tree_hull_kernel<KEYS>, dim3((unsigned)pt.tiles), dim3(HULL_NT), 0, s, a, pt, const_cast<Hull*>(pt.hull));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
     }
     hipLaunchKernelGGL((ragged_tile_kernel<DH, KEYS, FP8, 1>), grid, block, 0, s, a, pt);
   }
