@@ -749,7 +749,9 @@ wam_status wam_attn_tree(const wam_attn_tree_desc* desc, const wam_paged_cache* 
  * From the root on, the children of the present node are tried in order of their numbers: x is taken if
  *   u[x] s Q(x) < R(x),
  * where R = P and s = 1 at first, and each rejection replaces R by max(R - s Q, 0) and s by its sum (drawn = 0: Q is a one at x,
- * so R loses the rejected token).  When no child is left, next_token is drawn from R: the first v with R_0 + .. + R_v >
+ * so R loses the rejected token, and s is 1 minus what was rejected: p's rows are taken to sum to 1, without the entries that
+ * count as 0; of a row that does not, a second child is taken with another chance than R(x) / the sum of R).  When no child is
+ * left, next_token is drawn from R: the first v with R_0 + .. + R_v >
  * u_next[r] * (the sum of R) (the last with R_v > 0 if rounding leaves none); from P where the sum of R is 0, -1 where that
  * is 0 too.  With one-hot rows this is greedy verification.
  * u [T], u_next [R] in [0, 1) are the caller's random numbers.  Sums are in fp64.  Entries of p and q that are negative or NaN

@@ -4,8 +4,8 @@
 // if u s Q(x) < R(x), where R = P and s = 1 at first; after a rejection what is left of the target is
 // max(R - s Q, 0), its sum the new s.  With R_i = max(P_i - c Q_i, 0) that is max(P_i - (c + s) Q_i, 0) again, so c alone
 // says what is left, and only its sum takes a pass over the vocabulary.  (Drafts that were chosen, not drawn: Q is a one at
-// the child's token, so R is P without the tokens rejected so far, and s follows without a pass.)  The token after the last
-// node taken is drawn from R: the first one whose sum up to it exceeds u' times the whole.
+// the child's token, so R is P without the tokens rejected so far, and s, without a pass, one minus those.)  The token after
+// the last node taken is drawn from R: the first one whose sum up to it exceeds u' times the whole.
 //
 // Bound by reading the vocabulary's rows at the last node, and before that by the chain lengths -> nodes -> probabilities of
 // their tokens.  Every workgroup of a request walks its tree by itself (in each wavefront: 64 nodes at a time by

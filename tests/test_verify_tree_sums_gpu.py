@@ -1,10 +1,10 @@
-"""wam_verify_tree: the sums do not depend on the number of passes."""
+"""wam_verify_tree: the sums do not depend on the number of passes; rows that do not sum to one."""
 import numpy as np
 import pytest
 
 import branch_ref
 from gpu_helpers import log
-from test_verify_tree_gpu import check
+from test_verify_tree_gpu import OLD, check, run
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +24,13 @@ def test_a_sum_is_the_same_in_every_pass(T):
     log(f"verify order of a sum T={T}")
     assert branch_ref.verify(p[:3], q[:3], tokens, parent, [0.5] * 3, 0.5) == ([0], 4096)
     check(p, q, tokens, parent, np.full(T, 0.5), [0.5, 0.5], [0, 3, 4])
+
+
+def test_chosen_drafts_and_rows_that_do_not_sum_to_one():
+    """s is one minus what was rejected, whatever the row sums to: 0.55 (1 - 0.5) >= 0.25 rejects (0.55 * 0.375 would not)."""
+    p = np.array([[0.5, 0.25, 0.125, 0.0]] * 4, np.float32)
+    for u in (0.55, 0.45):
+        log(f"verify chosen, sum 0.875, u={u}")
+        check(p, None, [0, 0, 1, 2], [-1, 0, 0, 0], [0.0, 0.6, u, 0.9], [0.4], [0, 4])
+    path, _, _, _ = run(p, None, [0, 0, 1, 2], [-1, 0, 0, 0], [0.0, 0.6, 0.55, 0.9], [0.4], [0, 4])
+    assert path[:2] == [0, OLD]
