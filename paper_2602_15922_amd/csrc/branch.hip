@@ -28,7 +28,8 @@ WAM_DEV int wave_scan(int v) {
 // Fork.  Every workgroup finds in LDS which forks hold (the first to name a destination, which holds no page) and how many
 // of those before each need a page of their own; so one launch does it and none waits for another.  Rows that are
 // written belong to requests without pages and rows that are read to requests with some, so no order matters.  Bound by
-// latency (starts -> lengths -> table): 8 forks of 198 pages 3.0 us, 256 of up to 63 pages 4.9.
+// latency (starts -> lengths -> table; medians): 8 forks of 198 pages 4.1 us, 256 of up to 63 pages 5.8 (3.9 and 5.5 without the
+// look at the last page's entry, which an absent page needs).
 // ---------------------------------------------------------------------------------
 constexpr int FORK_NT = 256;
 
@@ -137,7 +138,8 @@ __global__ __launch_bounds__(FORK_NT) void page_fork_kernel(const PageForkArgs a
 
 // ---------------------------------------------------------------------------------
 // Copies of pages' first rows: 16-byte chunks of K and V in the order of the rows, four of each per thread on their way.  Bound
-// by memory: 256 copies of 0 to 127 rows, 16 heads of 128, 54.6 us for 247 MB (4.5 TB/s; a large copy reaches 4.85).
+// by memory: 256 copies of 0 to 127 rows, 16 heads of 128, 55.6 us for 247 MB (4.4 TB/s; a large copy reaches 4.85), of E4M3 33.7
+// for 126 (3.7: the exponents are a second trip, behind the stores).
 // ---------------------------------------------------------------------------------
 constexpr int COPY_NT = 256, COPY_PER = 4;
 
@@ -177,8 +179,10 @@ __global__ __launch_bounds__(COPY_NT) void page_copy_kernel(const PageCopyArgs a
 // the same), so it knows how many free pages lie below its share of the pool and lists its own; one launch does
 // it and none waits for another.  Pools of more bytes than LDS has go by segments, from the first on.
 // Bound by the instructions that one CU issues for all marks (16 wavefronts, 4 cycles each): so no lane is masked off, 8 rows' first 64
-// entries are on their way at once and then a longer row's, 512 at a time.  1000 requests that keep 0 to 1000 pages, 80000 of 144700 together: 28 us;
-// with lanes masked 40, a wavefront per row with atomic marks of a bit 44; 12 requests, 2224 pages 8.
+// entries are on their way at once and then a longer row's, 512 at a time.  That marks places past a row's end too, and the
+// wavefronts have their rows by number, not by length: 1000 requests that keep 0 to 1000 pages, 80078 of 144700 together, are 204288
+// places, 160 to 256 rounds of 64 to a wavefront.  They take 28 us; with lanes masked 40, a wavefront per row with atomic marks of a
+// bit 44; 12 requests, 2224 pages 7.4.
 // ---------------------------------------------------------------------------------
 constexpr int COLLECT_NT = 1024, COLLECT_SMALL = 32 << 10, COLLECT_LARGE = 152 << 10;
 
@@ -322,8 +326,8 @@ __global__ __launch_bounds__(COLLECT_NT) void page_collect_kernel(const PageColl
 // out), so a group of rows overwrites nothing that a later one reads, and its own loads end before its stores.
 // Bound by memory where lists are long (a group of 128 rows of 256 bytes, 32 KB, is on its way while the one before is stored;
 // the rows' places are looked up 1024 at a time), by the chain lengths -> numbers -> table -> row where they are short.  4 x 1576
-// of 3152 rows, 40 heads: 68 us for 258 MB (3.8 TB/s; groups of 256 rows 69.5, heads in a row on one XCD 68, marked as used once
-// 69.5); looked up as they are moved, nothing ahead, 166.  16 paths of 2 to 6 rows, 8 heads 3.9.
+// of 3152 rows, 40 heads: 67 us for 258 MB (3.8 TB/s; groups of 256 rows 69.5, heads in a row on one XCD 68, marked as used once
+// 69.5); looked up as they are moved, nothing ahead, 166; of E4M3 33 for 131 MB.  16 paths of 2 to 6 rows, 8 heads 3.3 (median).
 // ---------------------------------------------------------------------------------
 constexpr int MOVE_NT = 256, MOVE_PER = 8, MOVE_ROWS = 1024;
 

@@ -389,7 +389,8 @@ struct VerifyArgs {
 };
 // A pass for the last draw and one for each rejection that another child follows: chosen drafts and single ones need one in all;
 // of larger trees the more the more nodes they have.  48 trees of 8 to 32 nodes (17 on average; 1 to 4 passes), V = 100000: 2, 3, 4
-// rounds 51, 44, 36 us; a pass of the last workgroup takes 13 us, one more launch that nobody needs 3.5.
+// rounds 51, 44, 36 us; a pass of the last workgroup takes 13 us (V = 200000: 20), one more launch that nobody needs 3.5.  (By the
+// average alone: one tree of many rejected drafts among single tokens makes nearly all of its passes in the last workgroup.)
 inline int verify_rounds(const wam_verify_tree_desc& d) {
   if (!d.drawn || d.T <= 2 * (int64_t)d.R) return 1;
   return d.T <= 6 * (int64_t)d.R ? 2 : d.T <= 12 * (int64_t)d.R ? 3 : VERIFY_MAX_ROUNDS;
